@@ -10,9 +10,9 @@ Definitions.  With t <- t + 1, g = s G, c_i = 1 - beta_i^t:
   u <- beta1 u + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;  W <- W - lr ((u / c1) / (sqrt(v / c2) + eps) + wd W).
 The moments lie in one array [u | v], every tensor from a multiple of 128 elements on, zeros in between.
 
-Moments in 8 bits: 128 consecutive elements of a tensor are a block with one fp32 scale, the largest magnitude rounded to fp32.  A value over
-its scale, x in [0, 1], is one of  val(a) = 2^floor(a / 8) (1 + (a mod 8) / 8),  a = 0, -1, -2, ... : u has a sign and a >= -126, v has
-a >= -254, both have zero.  With theta in [0, 1), x between two neighbours val(a) <= x < val(a + 1) becomes the upper one if
+Moments in 8 bits: 128 consecutive elements of a tensor are a block with an exponent E, 2^E the least power of two that its largest magnitude, rounded
+to fp32, does not exceed.  A value over 2^E, x in [0, 1], is one of  val(a) = 2^floor(a / 8) (1 + (a mod 8) / 8),  a = 0, -1, -2, ... : u has a sign
+and a >= -126, v has a >= -254, both have zero.  With theta in [0, 1), x between two neighbours val(a) <= x < val(a + 1) becomes the upper one if
 (x - val(a)) / (val(a + 1) - val(a)) + theta >= 1.  Below the least value u takes that value if x over it plus theta is at least 1, else zero; v > 0
 always takes it.  theta = w / 2^17, w = ((t 0x9E3779B1 + i 0x85EBCA77) mod 2^32) >> 15 for element i of its tensor, and w + 2^16 mod 2^17 for v:
 the threshold of an element rotates from step to step, so that changes smaller than a step of the grid are not lost.  The step itself uses the
@@ -143,7 +143,7 @@ def work(case):
         rows = 2 * int(_distinct(c["tokens"], c["vocab"])) if c["add"] else c["vocab"]
         return {"bytes": 8 * c["tokens"] + _size(c["grad"]) * td + _size(c["out"]) * rows * c["d"], "flops": 2 * td}
     n = sum(p * q for p, q, _ in _shapes(c))
-    held = 8 if c["state"] == "f32" else 2 + 8 / BLOCK
+    held = 8 if c["state"] == "f32" else 2 + 2 / BLOCK
     nbytes = (2 * _size(c["w"]) + 2 * held) * n
     if c["state"] == "q8":                                         # the moments are given out in fp32 too
         nbytes += 8 * n
@@ -255,29 +255,27 @@ def prepare(case, seed):
 # ---- plain forms ------------------------------------------------------------------------------------------------------------------
 
 def _encode(x, w, signed):
-    """(codes, scales): codes from the leading bits of x over its scale, in 64 bits because the values lie next to borders."""
-    b = x.view(-1, BLOCK)
-    scale = b.abs().amax(1).float()
-    y = (b.abs() * (1.0 / scale.double())[:, None]).clamp(max=1.0)
+    """(codes, exponents): codes from the leading bits of x, in 64 bits because the values lie next to borders."""
+    b, w = x.view(-1, BLOCK), w.view(-1, BLOCK)
+    most = b.abs().amax(1, keepdim=True).float()
+    e = torch.where(most > 0, (most.view(torch.int32) - 1 >> 23) + 1 - 127, 0).long()
     least = 126 if signed else 254
-    bits = y.view(torch.int64)
-    a = ((bits >> 32) + w.view(-1, BLOCK)) >> 17
-    code = a - 8 * 1023 + least + 1
+    a = ((b.abs().view(torch.int64) >> 32) + w >> 17) - 8 * (e + 1023)
+    code = (a + least + 1).clamp(max=least + 1)
     low = 1.25 * 2.0 ** (-16 if signed else -32)
-    under = (y * (2.0 ** 17 / low)).long() + w.view(-1, BLOCK) >> 17 if signed else torch.ones_like(code)
+    y = b.abs() * (1023 - e << 52).view(torch.float64)
+    under = (y * (2.0 ** 17 / low)).long() + w >> 17 if signed else torch.ones_like(code)
     code = torch.where(y < low, under, code)
     code = torch.where(y > 0, code, torch.zeros_like(code))
     if signed:
         code = torch.where(b < 0, -code, code)
-    return code.to(torch.int16), scale
+    return code.to(torch.int16), e
 
 
-def _decode(codes, scale, signed):
-    n = codes.abs().double()
-    a = n - (127 if signed else 255)
-    e = torch.floor(a / 8)
-    y = torch.exp2(e) * (1 + (a - 8 * e) / 8) * torch.sign(codes)
-    return (y * scale.double()[:, None]).view(-1)
+def _decode(codes, e, signed):
+    n = codes.long().abs()
+    a = n - (127 if signed else 255) + 8 * (e + 1023)
+    return torch.where(n > 0, (a << 49).view(torch.float64) * torch.sign(codes), 0.0).view(-1)
 
 
 def _adamw_plain(state, g):
@@ -371,9 +369,10 @@ def _grid(x, theta, lo, zero_below):
 
 def _rounded(x, theta, lo, signed):
     b = x.view(-1, BLOCK)
-    scale = b.abs().amax(1, keepdim=True).float().double()
-    y = torch.where(scale > 0, b.abs() / scale, 0.0).clamp(max=1.0)
-    return (_grid(y, theta.view(-1, BLOCK), lo, signed) * scale * torch.sign(b)).view(-1)
+    m, e = torch.frexp(b.abs().amax(1, keepdim=True).float().double())
+    size = torch.ldexp(torch.ones_like(m), e - (m == 0.5).int())
+    y = (b.abs() / size).clamp(max=1.0)
+    return (_grid(y, theta.view(-1, BLOCK), lo, signed) * size * torch.sign(b)).view(-1)
 
 
 def exact(case, seed):
