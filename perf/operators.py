@@ -14,9 +14,9 @@ Moments in 8 bits: 128 consecutive elements of a tensor are a block with an expo
 to fp32, does not exceed.  A value over 2^E, x in [0, 1], is one of  val(a) = 2^floor(a / 8) (1 + (a mod 8) / 8),  a = 0, -1, -2, ... : u has a sign
 and a >= -126, v has a >= -254, both have zero.  With theta in [0, 1), x between two neighbours val(a) <= x < val(a + 1) becomes the upper one if
 (x - val(a)) / (val(a + 1) - val(a)) + theta >= 1.  Below the least value u takes that value if x over it plus theta is at least 1, else zero; v > 0
-always takes it.  theta = w / 2^17, w = ((t 0x9E3779B1 + i 0x85EBCA77) mod 2^32) >> 15 for element i of its tensor, and w + 2^16 mod 2^17 for v:
-the threshold of an element rotates from step to step, so that changes smaller than a step of the grid are not lost.  The step itself uses the
-moments before this rounding.  What is given as fp32 is taken with theta = 1/2.
+always takes it.  theta = w / 2^17, w the upper 17 bits of x for u and the lower 17 for v, where x mixes step and element i of the tensor in 32 bits:
+x = t 0x9E3779B1 + i 0xBB67AE85;  x = (x xor x >> 15) 0x6A09E667;  x = x xor x >> 14.  Rounding up in the right share of the steps, changes smaller than
+a step of the grid are not lost.  The step itself uses the moments before this rounding.  What is given as fp32 is taken with theta = 1/2.
 """
 import math
 
@@ -286,8 +286,10 @@ def _adamw_plain(state, g):
         g = g.double()
         u = BETA1 * _decode(*state["u"], True) + (1 - BETA1) * g
         v = BETA2 * _decode(*state["v"], False) + (1 - BETA2) * (g * g)
-        w = ((t * 0x9E3779B1 & 0xFFFFFFFF) + state["at"] * 0x85EBCA77 & 0xFFFFFFFF) >> 15
-        state["u"], state["v"] = _encode(u, w, True), _encode(v, w + (1 << 16) & 0x1FFFF, False)
+        x = (t * 0x9E3779B1 & 0xFFFFFFFF) + state["at"] * 0xBB67AE85 & 0xFFFFFFFF
+        x = (x ^ x >> 15) * 0x6A09E667 & 0xFFFFFFFF
+        x = x ^ x >> 14
+        state["u"], state["v"] = _encode(u, x >> 15, True), _encode(v, x & 0x1FFFF, False)
         u, v = u.float(), v.float()
         moments = torch.stack([_decode(*state["u"], True).float(), _decode(*state["v"], False).float()])
     else:
@@ -415,8 +417,10 @@ def exact(case, seed):
     w = s["w"].double()
     w = w - LR * (u / (1 - BETA1 ** t) / (torch.sqrt(v / (1 - BETA2 ** t)) + EPS) + s["decayed"].double() * w)
     if c["state"] == "q8":
-        turn = torch.remainder(t * 0x9E3779B1 + s["at"] * 0x85EBCA77, 2 ** 32) // 2 ** 15
-        u = _rounded(u, turn / 2.0 ** 17, -126, True)
-        v = _rounded(v, torch.remainder(turn / 2.0 ** 17 + 0.5, 1.0), -254, False)
+        x = torch.remainder(t * 0x9E3779B1 + torch.remainder(s["at"] * 0xBB67AE85, 2 ** 32), 2 ** 32)
+        x = torch.remainder(torch.bitwise_xor(x, x // 2 ** 15) * 0x6A09E667, 2 ** 32)
+        x = torch.bitwise_xor(x, x // 2 ** 14)
+        u = _rounded(u, (x // 2 ** 15) / 2.0 ** 17, -126, True)
+        v = _rounded(v, torch.remainder(x, 2 ** 17) / 2.0 ** 17, -254, False)
     out = [w, torch.stack([u, v])]
     return out + [clip] if kind == "step" else out
