@@ -328,6 +328,131 @@ int lordo_spectral_gap(lordo_ctx* ctx, const void* const* Src, int32_t src_dtype
 int lordo_profile_enable(lordo_ctx* ctx, int32_t on);
 int lordo_profile_read(lordo_ctx* ctx, int32_t kernel_class, double* total_ms, int64_t* launches, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * What a model has beside its projected matrices -- token embedding, output head, norm weights, biases -- is stepped at
+ * full rank by AdamW (Sec. 2, full-rank Adam; Sec. 5.1 trains with AdamW), together with what feeds that step: the
+ * embedding's gradient and the global norm that Alg. 1 clips by.  The conventions above hold; in addition
+ *   - a tensor is rows x cols, row-major and contiguous (a vector: 1 x cols), from any element on;
+ *   - the calls without a context work on the GPU that is current, where all their arrays have to live;
+ *   - a workspace is scratch between the start and the end of one call: calls that may run at the same time (two streams,
+ *     two recorded graphs) need one each.
+ * ------------------------------------------------------------------------------------------------------------- */
+#define LORDO_Q8  2            /* moments in 8 bits, see lordo_adamw_hparams.state_dtype */
+#define LORDO_I32 3            /* types of token ids */
+#define LORDO_I64 4
+#define LORDO_MAX_TOKENS     (1 << 26)
+#define LORDO_MAX_VOCAB      (1 << 22)
+#define LORDO_MAX_EMBED_COLS (1 << 20)
+
+typedef struct lordo_adamw lordo_adamw;
+
+/* One tensor: at most 2^38 elements; decay 1: the weight decay applies to it, 0: it does not (norm weights, biases). */
+typedef struct {
+  int64_t rows, cols;
+  int32_t decay;
+  int32_t reserved;              /* must be 0 */
+} lordo_tensor;
+
+/* Gradient of one tensor.
+ *   index NULL   dense: data is rows x cols of dtype; slots must be 0.
+ *   else         by rows, as lordo_embed_gradient_rows leaves it: data is slots x cols, row `index[k]` of it the gradient of row k of the
+ *                tensor (no row of data if that is outside [0, slots): gradient 0), and index[rows + j] the row of the tensor that row j of
+ *                data belongs to, or -1 where row j holds nothing.  rows <= LORDO_MAX_VOCAB, slots <= LORDO_MAX_TOKENS; with slots 0 data may be NULL. */
+typedef struct {
+  const void* data;
+  const int32_t* index;
+  int64_t rows, cols, slots;
+  int32_t dtype;                 /* LORDO_F32 or LORDO_BF16 */
+  int32_t reserved;              /* must be 0 */
+} lordo_grad;
+
+typedef struct {
+  double  beta1, beta2, eps;     /* as in lordo_hparams: in [0, 1), eps >= 0 outside the root */
+  double  weight_decay;          /* decoupled: W <- W - lr * weight_decay * W, >= 0 */
+  int32_t bias_correction;       /* as in lordo_hparams */
+  int32_t param_dtype;           /* LORDO_F32 or LORDO_BF16 storage of every W (formed in fp32, rounded to nearest-even once) */
+  int32_t state_dtype;           /* LORDO_F32, or LORDO_Q8: both moments in 8 bits.  128 consecutive elements of a tensor share an exponent E per
+                                    moment, 2^E the least power of two that their largest magnitude (in fp32) does not exceed; a value over 2^E is held as
+                                    val(a) = 2^floor(a/8) (1 + (a mod 8)/8), a = 0, -1, ... : u with a sign and a >= -126, v with a >= -254, or as 0.
+                                    It rounds up where the part of the way to the next value that it has gone, plus theta, reaches 1: theta =
+                                    w / 2^17, w the upper 17 bits of x for u and the lower 17 for v, in 32 bits x = t 0x9E3779B1 + i 0xBB67AE85 for element
+                                    i of its tensor at step t; x = (x xor x>>15) 0x6A09E667; x = x xor x>>14.  So it rounds up in the right share of
+                                    the steps, and changes below the grid (1 - beta2 of v a step) add up.
+                                    v > 0 is never held as 0; u below its least value takes it by the same rule, or 0.  W is updated from the moments before this rounding.  An infinity, a NaN or more than 2^127
+                                    makes the moments of its whole block NaN */
+  int32_t reserved;              /* must be 0 */
+} lordo_adamw_hparams;
+
+/* Bytes of arena lordo_adamw_init needs (host call): 8 bytes an element, or 2 and 2 bytes per 128 of them with LORDO_Q8. */
+int lordo_adamw_workspace_bytes(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams* hp, size_t* out_bytes);
+
+/* Create a context over n tensors; u = v = 0, t = 0.  arena as for lordo_init.  Synchronises `stream` before returning. */
+int lordo_adamw_init(lordo_adamw** out, const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams* hp,
+                     void* arena, size_t arena_bytes, void* stream);
+
+/* One AdamW step on every tensor (Sec. 2, full-rank Adam, with decoupled weight decay):
+ *   t <- t+1;  g = grad_scale * clip[1] * G;  u <- beta1 u + (1-beta1) g;  v <- beta2 v + (1-beta2) g*g;
+ *   W <- W - lr * ((u/c1) / (sqrt(v/c2) + eps) + weight_decay W),  c_i = 1-beta_i^t (1 if bias_correction == 0);
+ *   0/0 (eps = 0, no gradient so far) is 0.
+ *   W     host array of n device pointers, updated in place.
+ *   G     host array of n gradients of the tensors' rows and cols, read only.  Rows that a gradient by rows does not have get a gradient of
+ *         zero: their moments and weights decay as in any step.
+ *   clip  device, two floats as lordo_grad_norm leaves them, or NULL (coefficient 1).  With a coefficient that is not finite the whole step is
+ *         left out -- weights, moments and the step count on the device stay -- and latched for lordo_adamw_poll_status.
+ * The step count is kept as that of lordo_local_step: a recorded call counts its replays; lr and grad_scale are those of the recording.  A
+ * step beside a lordo_local_step shares nothing with it. */
+int lordo_adamw_step(lordo_adamw* ctx, void* const* W, const lordo_grad* G, double lr, double grad_scale, const float* clip, void* stream);
+
+/* The moments as one fp32 array [u | v]: tensor i begins, in each half, at the sum of the sizes before it, each rounded up to 128 elements;
+ * what lies between is zero.  An elementwise mean over workers of such arrays is the mean of every moment (Alg. 1, synchronisation).
+ *   lordo_adamw_sync_payload    *dev_ptr: the array itself, in the arena (averaged in place as with lordo_sync_payload); NULL with LORDO_Q8.
+ *                               *count: its elements
+ *   lordo_adamw_export_moments  dst[count] <- the moments (8-bit ones: the values they stand for, rounded to fp32)
+ *   lordo_adamw_import_moments  the moments <- src[count]; 8-bit ones with theta = 1/2 (what was exported comes back as it was) and |v| */
+int lordo_adamw_sync_payload(lordo_adamw* ctx, void** dev_ptr, size_t* count);
+int lordo_adamw_export_moments(lordo_adamw* ctx, float* dst, void* stream);
+int lordo_adamw_import_moments(lordo_adamw* ctx, const float* src, void* stream);
+
+/* Steps issued, as lordo_get_step / lordo_set_step. */
+int lordo_adamw_get_step(lordo_adamw* ctx, int64_t* t);
+int lordo_adamw_set_step(lordo_adamw* ctx, int64_t t);
+
+/* Synchronise `stream` and return LORDO_ENUMERIC if a step was left out since the last poll (cleared), else LORDO_OK. */
+int lordo_adamw_poll_status(lordo_adamw* ctx, void* stream);
+
+/* Frees host-side bookkeeping only.  NULL is allowed. */
+void lordo_adamw_destroy(lordo_adamw* ctx);
+
+/* Global norm over n gradients and the coefficient that clips by it (Alg. 1 clip), on the device:
+ *   out[0] = sqrt(sum of squares), formed in double;  out[1] = min(1, max_norm / norm), NaN if the norm is not finite.
+ *   G          gradients of any tensors (those of lordo_local_step too, whose grad_scale is out[1] read back)
+ *   max_norm   > 0; infinity: no clipping
+ *   workspace  device, LORDO_NORM_WORKSPACE_BYTES, 256-byte aligned
+ * The order of the sum depends on the sizes alone. */
+#define LORDO_NORM_WORKSPACE_BYTES 8192
+int lordo_grad_norm(const lordo_grad* G, int32_t n, double max_norm, float* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows of an embedding: out[j] = scale * table[ids[j]], j < tokens; a row of zeros for a token outside [0, vocab) (padding: -1, -100).
+ *   table  vocab x cols of table_dtype;  ids  tokens of ids_dtype (LORDO_I32, LORDO_I64);  out  tokens x cols of out_dtype.
+ * vocab <= LORDO_MAX_VOCAB, cols <= LORDO_MAX_EMBED_COLS, tokens <= LORDO_MAX_TOKENS (0: nothing is done), here and below. */
+int lordo_embed_lookup(const void* table, int32_t table_dtype, int64_t vocab, int64_t cols, const void* ids, int32_t ids_dtype,
+                       int64_t tokens, double scale, void* out, int32_t out_dtype, void* stream);
+
+/* Gradient of the lookup by sorted tokens: dW[k] = scale * sum over the tokens j with ids[j] = k of dY[j].  Tokens outside [0, vocab) and
+ * those equal to pad_id (-1: none) take no part.  Sums are fp32, over the tokens of a row in their order in pieces that the sorted ids alone fix: the same bits
+ * every time.
+ *   lordo_embed_gradient        dW vocab x cols: every row written (accumulate 0), or dW + the sum rounded once, where a token is (accumulate 1)
+ *   lordo_embed_gradient_rows   the form that lordo_adamw_step and lordo_grad_norm take as lordo_grad with slots = tokens: `rows` tokens x cols,
+ *                               of which one row is written per different token (the others stay as they were), `index` vocab + tokens
+ *   workspace  device, lordo_embed_workspace_bytes, 256-byte aligned */
+int lordo_embed_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols, size_t* out_bytes);
+int lordo_embed_gradient(const void* ids, int32_t ids_dtype, int64_t tokens, const void* dY, int32_t dy_dtype, int64_t vocab, int64_t cols,
+                         double scale, int64_t pad_id, int32_t accumulate, void* dW, int32_t dw_dtype,
+                         void* workspace, size_t workspace_bytes, void* stream);
+int lordo_embed_gradient_rows(const void* ids, int32_t ids_dtype, int64_t tokens, const void* dY, int32_t dy_dtype, int64_t vocab, int64_t cols,
+                              double scale, int64_t pad_id, void* rows, int32_t rows_dtype, int32_t* index,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
 const char* lordo_strerror(int code);
 
 /* Frees host-side bookkeeping only (the arena is the caller's).  NULL is allowed. */

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "liblordo.so")
-SOURCES = ["lordo.hip", "proj.hip", "gemm32.hip", "elementwise.hip"]
+SOURCES = ["lordo.hip", "proj.hip", "gemm32.hip", "elementwise.hip", "fullrank.hip", "embed.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 VALU forms

@@ -1,0 +1,100 @@
+// Shared pieces of the full-rank operators (fullrank.hip, embed.hip): element access at any alignment, and the entry points' guard
+// against C++ exceptions.
+#pragma once
+#include "../../include/lordo.h"
+#include "common.h"
+
+#include <cstdio>
+#include <new>
+
+namespace lordo {
+
+// Four consecutive elements from any element on: the hardware takes 8- and 16-byte accesses at 2- and 4-byte addresses, so only the type has to
+// say that it is aligned to an element.
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x4a __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4a __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bf16_value(uint32_t h) { return __uint_as_float(h << 16); }
+// nearest-even; a NaN stays a quiet one
+__device__ __forceinline__ uint32_t bf16_bits(float x) {
+  const uint32_t u = __float_as_uint(x);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;
+  return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+}
+
+template <bool BF>
+__device__ __forceinline__ float load_element(const void* p, int64_t i) {
+  if constexpr (BF) return bf16_value(reinterpret_cast<const uint16_t*>(p)[i]);
+  else return reinterpret_cast<const float*>(p)[i];
+}
+template <bool BF>
+__device__ __forceinline__ void store_element(void* p, int64_t i, float x) {
+  if constexpr (BF) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)bf16_bits(x);
+  else reinterpret_cast<float*>(p)[i] = x;
+}
+// STREAM: touched once a call, by one workgroup: kept out of the caches' way
+template <bool BF, bool STREAM>
+__device__ __forceinline__ void load_quad(const void* p, int64_t i, float (&x)[4]) {
+  if constexpr (BF) {
+    const u32x2u* q = reinterpret_cast<const u32x2u*>(reinterpret_cast<const uint16_t*>(p) + i);
+    u32x2u t;
+    if constexpr (STREAM) t = __builtin_nontemporal_load(q);
+    else t = *q;
+    x[0] = __uint_as_float(t.x << 16); x[1] = __uint_as_float(t.x & 0xffff0000u);
+    x[2] = __uint_as_float(t.y << 16); x[3] = __uint_as_float(t.y & 0xffff0000u);
+  } else {
+    const f32x4u* q = reinterpret_cast<const f32x4u*>(reinterpret_cast<const float*>(p) + i);
+    f32x4u t;
+    if constexpr (STREAM) t = __builtin_nontemporal_load(q);
+    else t = *q;
+    x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w;
+  }
+}
+template <bool BF, bool STREAM>
+__device__ __forceinline__ void store_quad(void* p, int64_t i, const float (&x)[4]) {
+  if constexpr (BF) {
+    u32x2u t;
+    t.x = bf16_bits(x[0]) | bf16_bits(x[1]) << 16;
+    t.y = bf16_bits(x[2]) | bf16_bits(x[3]) << 16;
+    u32x2u* q = reinterpret_cast<u32x2u*>(reinterpret_cast<uint16_t*>(p) + i);
+    if constexpr (STREAM) __builtin_nontemporal_store(t, q);
+    else *q = t;
+  } else {
+    f32x4u t = {x[0], x[1], x[2], x[3]};
+    f32x4u* q = reinterpret_cast<f32x4u*>(reinterpret_cast<float*>(p) + i);
+    if constexpr (STREAM) __builtin_nontemporal_store(t, q);
+    else *q = t;
+  }
+}
+
+// Which of up to 128 tensors chunk c belongs to: first[k] is the first chunk of tensor k (first[0] <= c).  Every lane compares its own entries, the
+// bits are counted: one round of loads instead of a chain of them.
+__device__ __forceinline__ int find_tensor(const int32_t* first, int count, int32_t c) {
+  const int lane = threadIdx.x & 63;
+  int k = __popcll(__ballot(lane < count && first[lane < count ? lane : 0] <= c));
+  if (count > 64) k += __popcll(__ballot(64 + lane < count && first[64 + lane < count ? 64 + lane : 0] <= c));
+  return k - 1;
+}
+
+// Nothing may leave a C entry point but a code.
+template <class F>
+int guarded(F&& f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    fprintf(stderr, "lordo: out of host memory\n");
+    return LORDO_ENOMEM;
+  } catch (...) {
+    return LORDO_EHIP;
+  }
+}
+inline int launched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return LORDO_OK;
+  fprintf(stderr, "lordo: %s failed: %s\n", what, hipGetErrorString(e));
+  return LORDO_EHIP;
+}
+
+}  // namespace lordo

@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "lib", "liblordo.so")
 
 OK, EINVAL, ENOMEM, EHIP, ESTATE, ENUMERIC = 0, -1, -2, -3, -4, -5
-F32, BF16 = 0, 1
+F32, BF16, Q8, I32, I64 = 0, 1, 2, 3, 4
 STATE_Q, STATE_U, STATE_V, STATE_ANCHOR, STATE_MOM, STATE_GLOW, STATE_NUPD, STATE_ERR, STATE_UPLINK, STATE_RITZ = range(10)
 
 EXPORTS = [
@@ -23,8 +23,14 @@ EXPORTS = [
     "lordo_profile_enable", "lordo_profile_read", "lordo_get_mssv", "lordo_refresh_subspace_local",
     "lordo_export_uplink", "lordo_outer_step_lowrank", "lordo_init_projection", "lordo_sync_payload",
     "lordo_get_stable_rank", "lordo_spectral_gap", "lordo_init_static",
+    "lordo_adamw_workspace_bytes", "lordo_adamw_init", "lordo_adamw_step", "lordo_adamw_sync_payload",
+    "lordo_adamw_export_moments", "lordo_adamw_import_moments", "lordo_adamw_get_step", "lordo_adamw_set_step",
+    "lordo_adamw_poll_status", "lordo_adamw_destroy", "lordo_grad_norm",
+    "lordo_embed_lookup", "lordo_embed_workspace_bytes", "lordo_embed_gradient", "lordo_embed_gradient_rows",
 ]
 STATIC_WORKSPACE_BYTES = 64 << 20
+NORM_WORKSPACE_BYTES = 8192
+MAX_TOKENS, MAX_VOCAB = 1 << 26, 1 << 22
 K_DOWN, K_ADAM, K_UP, K_OUTER, K_EXPORT, K_REFRESH = range(6)
 
 
@@ -53,6 +59,24 @@ def hparams(beta1=0.9, beta2=0.999, eps=1e-8, bias_correction=True, outer_lr=1.0
     return HParams(beta1, beta2, eps, int(bias_correction), qhm_mode, omega, int(error_feedback),
                    int(outer_nesterov), outer_lr, outer_momentum, power_iters, orth_passes, grad_dtype, int(uplink_buffer),
                    int(rayleigh_ritz), int(param_dtype), int(err_dtype), 0, int(seed))
+
+
+class Tensor(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("decay", C.c_int32), ("reserved", C.c_int32)]
+
+
+class Grad(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("index", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("slots", C.c_int64),
+                ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class AdamWHParams(C.Structure):
+    _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("bias_correction", C.c_int32), ("param_dtype", C.c_int32), ("state_dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+def adamw_hparams(beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, bias_correction=True, param_dtype=F32, state_dtype=F32) -> AdamWHParams:
+    return AdamWHParams(beta1, beta2, eps, weight_decay, int(bias_correction), int(param_dtype), int(state_dtype), 0)
 
 
 class LordoError(RuntimeError):
@@ -99,8 +123,25 @@ def load() -> C.CDLL:
     lib.lordo_strerror.restype = C.c_char_p
     lib.lordo_destroy.argtypes = [vp]
     lib.lordo_destroy.restype = None
+    lib.lordo_adamw_workspace_bytes.argtypes = [C.POINTER(Tensor), C.c_int32, C.POINTER(AdamWHParams), C.POINTER(C.c_size_t)]
+    lib.lordo_adamw_init.argtypes = [C.POINTER(vp), C.POINTER(Tensor), C.c_int32, C.POINTER(AdamWHParams), vp, C.c_size_t, vp]
+    lib.lordo_adamw_step.argtypes = [vp, vpp, C.POINTER(Grad), C.c_double, C.c_double, vp, vp]
+    lib.lordo_adamw_sync_payload.argtypes = [vp, vpp, C.POINTER(C.c_size_t)]
+    lib.lordo_adamw_export_moments.argtypes = [vp, vp, vp]
+    lib.lordo_adamw_import_moments.argtypes = [vp, vp, vp]
+    lib.lordo_adamw_get_step.argtypes = [vp, C.POINTER(C.c_int64)]
+    lib.lordo_adamw_set_step.argtypes = [vp, C.c_int64]
+    lib.lordo_adamw_poll_status.argtypes = [vp, vp]
+    lib.lordo_adamw_destroy.argtypes = [vp]
+    lib.lordo_adamw_destroy.restype = None
+    lib.lordo_grad_norm.argtypes = [C.POINTER(Grad), C.c_int32, C.c_double, vp, vp, C.c_size_t, vp]
+    i32, i64, f64, size = C.c_int32, C.c_int64, C.c_double, C.c_size_t
+    lib.lordo_embed_lookup.argtypes = [vp, i32, i64, i64, vp, i32, i64, f64, vp, i32, vp]
+    lib.lordo_embed_workspace_bytes.argtypes = [i64, i64, i64, C.POINTER(C.c_size_t)]
+    lib.lordo_embed_gradient.argtypes = [vp, i32, i64, vp, i32, i64, i64, f64, i64, i32, vp, i32, vp, size, vp]
+    lib.lordo_embed_gradient_rows.argtypes = [vp, i32, i64, vp, i32, i64, i64, f64, i64, vp, i32, vp, vp, size, vp]
     for name in EXPORTS:
-        if name not in ("lordo_strerror", "lordo_destroy"):
+        if name not in ("lordo_strerror", "lordo_destroy", "lordo_adamw_destroy"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -349,3 +390,263 @@ class Lordo:
             self.close()
         except Exception:
             pass
+
+
+# ---- what a model has beside its projected matrices: AdamW, gradient norm, token embedding ------------------------------
+
+def _torch():
+    import torch
+    return torch
+
+
+def _same_device(*tensors):
+    """The one GPU all of them are on, which has to be current: the calls without a context enqueue there."""
+    dev = tensors[0].device
+    if dev.type != "cuda" or any(t.device != dev for t in tensors):
+        raise ValueError("expected CUDA tensors on one device")
+    if dev.index != _torch().cuda.current_device():
+        raise ValueError(f"tensors are on {dev}, which is not the current device")
+    return dev
+
+
+def _stream_of(torch):
+    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _float_code(t, torch):
+    if t.dtype == torch.float32:
+        return F32
+    if t.dtype == torch.bfloat16:
+        return BF16
+    raise ValueError(f"expected a float32 or bfloat16 tensor, got {t.dtype}")
+
+
+def _rows_cols(t):
+    return (t.shape[0], t.shape[1]) if t.dim() == 2 else (1, t.numel())
+
+
+class RowGrad:
+    """Gradient of a (vocab, cols) tensor by rows, as embed_gradient_rows returns it: `rows` (slots, cols), `index` int32 (vocab + slots): the row of
+    `rows` of each row of the tensor, or -1, and behind them the row of the tensor of each row of `rows`, or -1.  `rows` holds nothing where that is -1."""
+
+    def __init__(self, rows, index, vocab):
+        if rows.dim() != 2 or index.dim() != 1 or index.numel() != vocab + rows.shape[0] or index.dtype != _torch().int32:
+            raise ValueError("expected rows (slots, cols) and an int32 index of vocab + slots")
+        self.rows, self.index, self.vocab = rows, index, vocab
+
+    @property
+    def shape(self):
+        return (self.vocab, self.rows.shape[1])
+
+
+class GradList:
+    """A list of gradients (tensors of one or two dimensions, RowGrads) validated once, reusable across calls; keeps them alive."""
+
+    def __init__(self, grads):
+        torch = _torch()
+        self.grads = list(grads)
+        if not self.grads:
+            raise ValueError("no gradients")
+        self.arr = (Grad * len(self.grads))()
+        flat = []
+        for a, g in zip(self.arr, self.grads):
+            if isinstance(g, RowGrad):
+                data, a.index, a.slots = g.rows, g.index.data_ptr(), g.rows.shape[0]
+                flat.append(g.index)
+                if not g.index.is_contiguous():
+                    raise ValueError("expected contiguous gradients")
+            else:
+                data = g
+            a.rows, a.cols = g.shape if isinstance(g, RowGrad) else _rows_cols(g)
+            a.data, a.dtype = data.data_ptr() or None, _float_code(data, torch)
+            if not data.is_contiguous():
+                raise ValueError("expected contiguous gradients")
+            flat.append(data)
+        self.device = flat[0].device
+        if self.device.type != "cuda" or any(t.device != self.device for t in flat):
+            raise ValueError("expected CUDA tensors on one device")
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def grad_list(grads) -> GradList:
+    return grads if isinstance(grads, GradList) else GradList(grads)
+
+
+def grad_norm(grads, max_norm=float("inf"), out=None):
+    """Tensor of two floats on the device: the norm over all gradients, and min(1, max_norm / norm) (Alg. 1 clip; NaN if the norm is not finite).
+    AdamW.local_step takes it as `clip`; Lordo.local_step takes its second value, read back, as grad_scale."""
+    torch = _torch()
+    grads = grad_list(grads)
+    if grads.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {grads.device}, which is not the current device")
+    if out is None:
+        out = torch.empty(2, dtype=torch.float32, device=grads.device)
+    elif out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous() or out.device != grads.device:
+        raise ValueError("expected a contiguous float32 tensor of two elements on the gradients' device")
+    ws = torch.empty(NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=grads.device)
+    _check(load().lordo_grad_norm(grads.arr, len(grads), float(max_norm), C.c_void_p(out.data_ptr()), C.c_void_p(ws.data_ptr()), NORM_WORKSPACE_BYTES,
+                                  _stream_of(torch)))
+    return out
+
+
+class AdamW:
+    """AdamW over the tensors that are not projected.  `shapes`: (rows, cols) or (rows, cols, decay) of each, a vector as (1, cols); `W` is a list of
+    torch CUDA tensors of those sizes, contiguous, of hp.param_dtype; gradients are tensors or RowGrads."""
+
+    def __init__(self, shapes, hp: AdamWHParams, torch, device=None):
+        self.lib, self.torch, self.hp = load(), torch, hp
+        self.ctx = C.c_void_p()
+        self.shapes = [tuple(sh) for sh in shapes]
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        if self.device.index != torch.cuda.current_device():
+            raise ValueError(f"{self.device} is not the current device")
+        arr = (Tensor * len(self.shapes))()
+        for a, sh in zip(arr, self.shapes):
+            a.rows, a.cols, a.decay = sh[0], sh[1], sh[2] if len(sh) > 2 else 1
+        nbytes = C.c_size_t(0)
+        _check(self.lib.lordo_adamw_workspace_bytes(arr, len(arr), C.byref(hp), C.byref(nbytes)))
+        self.arena = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
+        base = (self.arena.data_ptr() + 255) // 256 * 256
+        _check(self.lib.lordo_adamw_init(C.byref(self.ctx), arr, len(arr), C.byref(hp), C.c_void_p(base), nbytes.value, self._stream()))
+
+    def _stream(self):
+        return _stream_of(self.torch)
+
+    def ptrs(self, W) -> PtrList:
+        """Validate the list of weights once and freeze its pointers for repeated calls."""
+        if isinstance(W, PtrList):
+            return W
+        dtype = self.torch.bfloat16 if self.hp.param_dtype == BF16 else self.torch.float32
+        if len(W) != len(self.shapes):
+            raise ValueError("one tensor per shape expected")
+        for t, sh in zip(W, self.shapes):
+            if _rows_cols(t) != sh[:2] or t.dtype != dtype or not t.is_contiguous() or t.device != self.device:
+                raise ValueError(f"expected a contiguous {dtype} tensor of shape {sh[:2]} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return PtrList(list(W), _ptr_array(W))
+
+    def local_step(self, W, G, lr, grad_scale=1.0, clip=None):
+        """One step; the gradient is grad_scale * clip[1] * G (clip: what grad_norm returned, or None)."""
+        W, G = self.ptrs(W), grad_list(G)
+        if len(G) != len(self.shapes) or G.device != self.device:
+            raise ValueError(f"expected one gradient per shape on {self.device}")
+        if clip is not None and (clip.dtype != self.torch.float32 or clip.numel() != 2 or not clip.is_contiguous() or clip.device != self.device):
+            raise ValueError("clip: expected the two floats of grad_norm")
+        _check(self.lib.lordo_adamw_step(self.ctx, W.arr, G.arr, float(lr), float(grad_scale),
+                                         None if clip is None else C.c_void_p(clip.data_ptr()), self._stream()))
+
+    def _moments(self):
+        ptr, count = C.c_void_p(), C.c_size_t()
+        _check(self.lib.lordo_adamw_sync_payload(self.ctx, C.byref(ptr), C.byref(count)))
+        return ptr.value, count.value
+
+    def sync_payload(self):
+        """The moments [u | v] in the arena as a (2, n) fp32 view (Alg. 1 synchronisation); tensor i starts at a multiple of 128 elements, in the order of
+        the shapes.  Moments in 8 bits have none: export_moments, import_moments."""
+        ptr, count = self._moments()
+        if ptr is None:
+            raise ValueError("moments in 8 bits have no fp32 array: use export_moments and import_moments")
+        off = ptr - self.arena.data_ptr()
+        return self.arena[off:off + 4 * count].view(self.torch.float32).view(2, -1)
+
+    def _check_moments(self, t, count):
+        if t.dtype != self.torch.float32 or t.numel() != count or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"expected a contiguous float32 tensor of {count} elements on {self.device}")
+
+    def export_moments(self, out=None):
+        count = self._moments()[1]
+        if out is None:
+            out = self.torch.empty((2, count // 2), dtype=self.torch.float32, device=self.device)
+        self._check_moments(out, count)
+        _check(self.lib.lordo_adamw_export_moments(self.ctx, C.c_void_p(out.data_ptr()), self._stream()))
+        return out
+
+    def import_moments(self, src):
+        self._check_moments(src, self._moments()[1])
+        _check(self.lib.lordo_adamw_import_moments(self.ctx, C.c_void_p(src.data_ptr()), self._stream()))
+
+    @property
+    def step(self):
+        t = C.c_int64(0)
+        _check(self.lib.lordo_adamw_get_step(self.ctx, C.byref(t)))
+        return t.value
+
+    @step.setter
+    def step(self, t):
+        _check(self.lib.lordo_adamw_set_step(self.ctx, int(t)))
+
+    def poll_status(self):
+        """Raises (ENUMERIC) if a step was left out since the last poll because the clip coefficient was not finite."""
+        _check(self.lib.lordo_adamw_poll_status(self.ctx, self._stream()))
+
+    def close(self):
+        if self.ctx:
+            self.lib.lordo_adamw_destroy(self.ctx)
+            self.ctx = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _ids(ids, torch):
+    if ids.dtype not in (torch.int64, torch.int32) or not ids.is_contiguous():
+        raise ValueError("expected contiguous int32 or int64 token ids")
+    return C.c_void_p(ids.data_ptr()), I64 if ids.dtype == torch.int64 else I32, ids.numel()
+
+
+def embed_lookup(table, ids, scale=1.0, out=None, dtype=None):
+    """out[...] = scale * table[ids[...]] as a tensor of ids.shape + (cols,), of `dtype` (the table's if None); zeros for ids outside [0, vocab)."""
+    torch = _torch()
+    if table.dim() != 2 or not table.is_contiguous():
+        raise ValueError("expected a contiguous (vocab, cols) table")
+    p, code, n = _ids(ids, torch)
+    want = tuple(ids.shape) + (table.shape[1],)
+    if out is None:
+        out = torch.empty(want, dtype=dtype or table.dtype, device=table.device)
+    elif tuple(out.shape) != want or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"expected a contiguous output of shape {want}")
+    _same_device(table, ids, out)
+    _check(load().lordo_embed_lookup(C.c_void_p(table.data_ptr()), _float_code(table, torch), table.shape[0], table.shape[1], p, code, n, float(scale),
+                                     C.c_void_p(out.data_ptr()), _float_code(out, torch), _stream_of(torch)))
+    return out
+
+
+def _gradient_args(ids, dy, vocab, torch):
+    cols = dy.shape[-1]
+    if tuple(dy.shape[:-1]) != tuple(ids.shape) or not dy.is_contiguous():
+        raise ValueError(f"expected a contiguous gradient of shape {tuple(ids.shape) + (cols,)}")
+    size = C.c_size_t(0)
+    _check(load().lordo_embed_workspace_bytes(ids.numel(), vocab, cols, C.byref(size)))
+    return cols, size.value, torch.empty(size.value, dtype=torch.uint8, device=dy.device)
+
+
+def embed_gradient(ids, dy, out, scale=1.0, pad_id=-1, accumulate=False):
+    """Dense gradient of embed_lookup: out (vocab, cols) <- scale * sum of dy over the tokens of each row, added to out with accumulate."""
+    torch = _torch()
+    if out.dim() != 2 or not out.is_contiguous() or dy.shape[-1] != out.shape[1]:
+        raise ValueError("expected a contiguous (vocab, cols) output")
+    _same_device(ids, dy, out)
+    p, code, n = _ids(ids, torch)
+    cols, size, ws = _gradient_args(ids, dy, out.shape[0], torch)
+    _check(load().lordo_embed_gradient(p, code, n, C.c_void_p(dy.data_ptr()), _float_code(dy, torch), out.shape[0], cols, float(scale), int(pad_id),
+                                       int(accumulate), C.c_void_p(out.data_ptr()), _float_code(out, torch), C.c_void_p(ws.data_ptr()), size,
+                                       _stream_of(torch)))
+    return out
+
+
+def embed_gradient_rows(ids, dy, vocab, scale=1.0, pad_id=-1, dtype=None) -> RowGrad:
+    """Gradient of embed_lookup by rows, for AdamW.local_step and grad_norm: one row per different token, of `dtype` (float32 if None)."""
+    torch = _torch()
+    _same_device(ids, dy)
+    p, code, n = _ids(ids, torch)
+    cols, size, ws = _gradient_args(ids, dy, vocab, torch)
+    rows = torch.empty((n, cols), dtype=dtype or torch.float32, device=dy.device)
+    index = torch.empty(vocab + n, dtype=torch.int32, device=dy.device)
+    _check(load().lordo_embed_gradient_rows(p, code, n, C.c_void_p(dy.data_ptr()), _float_code(dy, torch), vocab, cols, float(scale), int(pad_id),
+                                            C.c_void_p(rows.data_ptr()), _float_code(rows, torch), C.c_void_p(index.data_ptr()),
+                                            C.c_void_p(ws.data_ptr()), size, _stream_of(torch)))
+    return RowGrad(rows, index, vocab)
