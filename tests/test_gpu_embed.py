@@ -113,15 +113,16 @@ def test_gradient_by_rows(torch, tokens, vocab, cols, kind):
         assert by_rows.shape == (vocab, cols)
 
 
-@pytest.mark.parametrize("tokens, vocab", [(9000, 300), (20000, 70000), (40000, 1000), (70001, 32000)])
+@pytest.mark.parametrize("tokens, vocab, cols", [(8192, 300, 20), (8193, 300, 20), (20000, 70000, 20), (40000, 1000, 300), (70001, 32000, 20), (5000, (1 << 21) + 5, 2),
+                                                 (9000, 1 << 22, 2), (600001, 5000, 1), (12000, 1, 5)])
 @pytest.mark.parametrize("kind", ["zipf", "all", "mixed"])
-def test_gradient_of_many_tokens(torch, tokens, vocab, kind):
-    """Sums that cross many pieces, ids of more than 16 bits."""
+def test_gradient_of_many_tokens(torch, tokens, vocab, cols, kind):
+    """Sums that cross many pieces, ids of up to 22 bits."""
     from paper_2602_04396_amd import lordo
     ids = _ids(torch, kind, tokens, vocab)
-    dy = torch.randn(tokens, 20, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    dy = torch.randn(tokens, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
     dev = torch.tensor(ids).cuda()
-    out = lordo.embed_gradient(dev, dy, torch.full((vocab, 20), 9.0, device="cuda"))
+    out = lordo.embed_gradient(dev, dy, torch.full((vocab, cols), 9.0, device="cuda"))
     total, size, count = ref.embed_gradient(ids, dy.double().cpu().numpy(), vocab, 1.0)
     assert np.all(np.abs(out.double().cpu().numpy() - total) <= ref.embed_bound(total, size, count, False))
     assert torch.equal(lordo.embed_gradient(dev, dy, torch.empty_like(out)), out)
