@@ -222,48 +222,12 @@ __global__ __launch_bounds__(1024) void k_place(Ids ids, Sorted in, Sorted out, 
   }
 }
 
-typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
-
 struct GradOut {
   void* dst;                          // vocab x cols, or rows in the order of the first of their tokens
   int32_t* index;                     // rows: row of dst of an id, behind it the id of a row of dst (null: dense)
   float* part;                        // two partial rows a tile: of the run it goes on with, and of the one that goes on behind it
   float scale;
   int32_t add;
-};
-
-// VEC consecutive elements of a row of a gradient or output, from any element on, as they are stored.
-template <bool BF, int VEC>
-struct Piece;
-template <>
-struct Piece<false, 4> {
-  f32x4u v;
-  __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const f32x4u*>(reinterpret_cast<const float*>(p) + at); }
-  __device__ __forceinline__ float value(int e) const { return v[e]; }
-};
-template <>
-struct Piece<true, 4> {
-  u32x2u v;
-  __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const u32x2u*>(reinterpret_cast<const uint16_t*>(p) + at); }
-  __device__ __forceinline__ float value(int e) const { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
-};
-template <>
-struct Piece<true, 8> {
-  u32x4u v;
-  __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const u32x4u*>(reinterpret_cast<const uint16_t*>(p) + at); }
-  __device__ __forceinline__ float value(int e) const { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
-};
-template <>
-struct Piece<false, 8> {
-  Piece<false, 4> v[2];
-  __device__ __forceinline__ void load(const void* p, int64_t at) { v[0].load(p, at); v[1].load(p, at + 4); }
-  __device__ __forceinline__ float value(int e) const { return v[e / 4].value(e & 3); }
-};
-template <bool BF>
-struct Piece<BF, 1> {
-  float v;
-  __device__ __forceinline__ void load(const void* p, int64_t at) { v = load_element<BF>(p, at); }
-  __device__ __forceinline__ float value(int) const { return v; }
 };
 
 // Elements skip ... VEC - 1 of a piece (what comes before them is the neighbour's).

@@ -13,6 +13,7 @@ namespace lordo {
 // say that it is aligned to an element.
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4a __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4a __attribute__((ext_vector_type(4)));
 
@@ -69,13 +70,51 @@ __device__ __forceinline__ void store_quad(void* p, int64_t i, const float (&x)[
   }
 }
 
-// Which of up to 128 tensors chunk c belongs to: first[k] is the first chunk of tensor k (first[0] <= c).  Every lane compares its own entries, the
+// VEC consecutive elements from any element on, as they are stored.
+template <bool BF, int VEC>
+struct Piece;
+template <>
+struct Piece<false, 4> {
+  f32x4u v;
+  __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const f32x4u*>(reinterpret_cast<const float*>(p) + at); }
+  __device__ __forceinline__ float value(int e) const { return v[e]; }
+};
+template <>
+struct Piece<true, 4> {
+  u32x2u v;
+  __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const u32x2u*>(reinterpret_cast<const uint16_t*>(p) + at); }
+  __device__ __forceinline__ float value(int e) const { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
+};
+template <>
+struct Piece<true, 8> {
+  u32x4u v;
+  __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const u32x4u*>(reinterpret_cast<const uint16_t*>(p) + at); }
+  __device__ __forceinline__ float value(int e) const { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
+};
+template <>
+struct Piece<false, 8> {
+  Piece<false, 4> v[2];
+  __device__ __forceinline__ void load(const void* p, int64_t at) { v[0].load(p, at); v[1].load(p, at + 4); }
+  __device__ __forceinline__ float value(int e) const { return v[e / 4].value(e & 3); }
+};
+template <bool BF>
+struct Piece<BF, 1> {
+  float v;
+  __device__ __forceinline__ void load(const void* p, int64_t at) { v = load_element<BF>(p, at); }
+  __device__ __forceinline__ float value(int) const { return v; }
+};
+
+// Which of up to 256 tensors chunk c belongs to: first[k] is the first chunk of tensor k (first[0] <= c).  Every lane compares its own entries, the
 // bits are counted: one round of loads instead of a chain of them.
 __device__ __forceinline__ int find_tensor(const int32_t* first, int count, int32_t c) {
   const int lane = threadIdx.x & 63;
-  int k = __popcll(__ballot(lane < count && first[lane < count ? lane : 0] <= c));
-  if (count > 64) k += __popcll(__ballot(64 + lane < count && first[64 + lane < count ? 64 + lane : 0] <= c));
-  return k - 1;
+  int32_t x[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) x[q] = first[64 * q + lane < count ? 64 * q + lane : 0];
+  int k = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) k += __popcll(__ballot(64 * q + lane < count && x[q] <= c));
+  return __builtin_amdgcn_readfirstlane(k - 1);
 }
 
 // Nothing may leave a C entry point but a code.

@@ -2,7 +2,7 @@
 // or in 8 bits, and the global gradient norm with its clip coefficient.
 //
 //   k_adamw<WBF, Q8>   t <- t + 1; u <- b1 u + (1 - b1) s g; v <- b2 v + (1 - b2)(s g)^2; W <- W - lr ((u / c1) / (sqrt(v / c2) + eps) + wd W)
-//   k_adamw_advance    step count and bias corrections of the next step
+//                      and, by its last workgroup, step count and bias corrections of the next step
 //   k_moments          8-bit moments <-> the fp32 array [u | v]
 //   k_norm_part, k_norm_sum   sqrt(sum g^2) and min(1, max / norm)
 #include "fullrank.h"
@@ -16,10 +16,12 @@ namespace lordo {
 
 constexpr int64_t ADAMW_CHUNK = 4096;    // elements of one tensor that a workgroup takes
 constexpr int Q8_BLOCK = 128;            // elements that share a scale
-constexpr int ADAMW_GROUP = 120;         // tensors of one launch: their pointers travel in the kernel arguments (below 4 KiB)
-constexpr int NORM_GROUP = 64;
-constexpr int64_t NORM_CHUNK = 8192;
+constexpr int GROUP = 200;               // tensors of one launch, and gradients by rows among them: their pointers travel in the kernel arguments (below 4 KiB)
+constexpr int GROUP_ROWS = 8;
+constexpr int64_t NORM_CHUNK = 16384;
 constexpr int NORM_BLOCKS = 1024;
+constexpr int NORM_ALONE = 6;           // chunks that one workgroup takes without a second launch
+constexpr int COUNTERS = 16;             // of finished workgroups, 128 bytes apart, behind them the one of finished counters
 
 // What the plan knows of a tensor (device memory, written once).
 struct AdamwTensor {
@@ -32,17 +34,23 @@ struct AdamwState {
   uint8_t *cu, *cv;        // their codes and
   uint8_t *eu, *ev;        // the exponents of the blocks
 };
+// A gradient by rows of a launch.
+struct RowsOf {
+  const int32_t* index;                   // row of the tensor -> row of the data, or none if outside [0, slots); behind them row of the data -> of the tensor
+  int32_t slots;
+};
+constexpr uint8_t G_BF16 = 1, G_ROWS = 2;  // bits of what a gradient is; above them its entry of `rows`
 struct AdamwArgs {
-  void* w[ADAMW_GROUP];
-  const void* g[ADAMW_GROUP];
-  const int32_t* index[ADAMW_GROUP];      // row of the vocabulary -> row of g, or -1 (null: g is dense)
-  int32_t slots[ADAMW_GROUP];             // rows of g
-  uint8_t g_bf16[ADAMW_GROUP];
-  int32_t count;
+  void* w[GROUP];
+  const void* g[GROUP];
+  uint8_t kind[GROUP];
+  RowsOf rows[GROUP_ROWS];
+  int32_t count, advance;                 // advance: the last launch of the step moves its count on
   float b1, omb1, b2, omb2, eps, lr, wd;
   double b1d, omb1d, b2d, omb2d, scale;
   const float* coef;                      // clip coefficient on the device (null: 1)
-  const StepDev* step;
+  StepDev* step;
+  int32_t* flag;                          // latch of steps left out, and the counters 128 bytes behind it
   const AdamwTensor* tensors;             // of this group
   const int32_t* first;                   // chunks before each
   AdamwState st;
@@ -128,131 +136,199 @@ __device__ __forceinline__ void q8_store(const AdamwState& st, int64_t at, bool 
   }
 }
 
-// Gradient of four elements from i on, `cnt` of them there: dense, or by rows of a vocabulary of which few are there.
-__device__ __forceinline__ void load_gradient(const void* g, const int32_t* index, int32_t slots, bool bf16, int64_t cols, int64_t row0, int64_t col0,
-                                              int64_t i, int64_t ahead, int cnt, float (&x)[4]) {
-  x[0] = x[1] = x[2] = x[3] = 0.f;
-  if (index == nullptr) {
-    if (cnt == 4) {
-      if (bf16) load_quad<true, true>(g, i, x);
-      else load_quad<false, true>(g, i, x);
-    } else {
-      for (int e = 0; e < cnt; ++e) x[e] = bf16 ? load_element<true>(g, i + e) : load_element<false>(g, i + e);
-    }
-    return;
-  }
-  // i = (row0, col0) + ahead, ahead < ADAMW_CHUNK: 32-bit arithmetic once col0 + ahead is below 2^32
+// Gradient of four elements from i on, `cnt` of them there, of a tensor whose gradient is held by rows: i = (row0, col0) + ahead.
+__device__ __forceinline__ void load_rows(const void* g, const RowsOf& rows, bool bf16, int64_t cols, int64_t row0, int64_t col0, int64_t ahead, int cnt,
+                                          float (&x)[4]) {
   const uint64_t c = (uint64_t)(col0 + ahead);
   int64_t row, col;
-  if (cols < (int64_t(1) << 31)) {
+  if (cols < (int64_t(1) << 31)) {                     // then c is below 2^32
     const uint32_t q = (uint32_t)c / (uint32_t)cols;
     row = row0 + q; col = (int64_t)((uint32_t)c - q * (uint32_t)cols);
   } else {
     row = row0 + (int64_t)(c / (uint64_t)cols); col = (int64_t)(c % (uint64_t)cols);
   }
   if (cnt == 4 && col + 4 <= cols) {
-    const int32_t slot = index[row];
-    if ((uint32_t)slot < (uint32_t)slots) {
+    const int32_t slot = rows.index[row];
+    if ((uint32_t)slot < (uint32_t)rows.slots) {
       if (bf16) load_quad<true, true>(g, slot * cols + col, x);
       else load_quad<false, true>(g, slot * cols + col, x);
     }
     return;
   }
-  for (int e = 0; e < cnt; ++e) {
-    const int32_t slot = index[row];
-    if ((uint32_t)slot < (uint32_t)slots) x[e] = bf16 ? load_element<true>(g, slot * cols + col) : load_element<false>(g, slot * cols + col);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e >= cnt) break;
+    const int32_t slot = rows.index[row];
+    if ((uint32_t)slot < (uint32_t)rows.slots) x[e] = bf16 ? load_element<true>(g, slot * cols + col) : load_element<false>(g, slot * cols + col);
     if (++col == cols) { col = 0; ++row; }
   }
 }
 
-template <bool WBF, bool Q8>
-__global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
-  const int32_t c = a.first[0] + (int32_t)blockIdx.x;
-  const int k = __builtin_amdgcn_readfirstlane(find_tensor(a.first, a.count, c));
-  const AdamwTensor t = a.tensors[k];
-  const float coef = a.coef ? *a.coef : 1.f;
-  if (!(fabsf(coef) < INFINITY)) return;             // the norm was not finite: this step is left out (k_adamw_advance latches it)
-  const double scale_d = a.scale * (double)coef;
-  const float scale = (float)scale_d;
-  const int64_t base = (int64_t)(c - a.first[k]) * ADAMW_CHUNK;
-  void* const w = a.w[k];
-  const void* const g = a.g[k];
-  const int32_t* const index = a.index[k];
-  const int32_t slots = a.slots[k];
-  const bool g_bf16 = a.g_bf16[k] != 0;
-  const float inv_c1 = a.step->next_inv_c1, inv_c2 = a.step->next_inv_c2, wd = t.decay ? a.wd : 0.f;
-  const uint32_t turn = (uint32_t)(a.step->t + 1) * STEP_TURN;
-  int64_t row0 = 0, col0 = 0;
-  if (index) { row0 = base / t.cols; col0 = base - row0 * t.cols; }
+// What a thread holds of four elements of W, G, u and v.
+template <bool Q8> struct Quad;
+template <> struct Quad<false> {
+  float x[4], g[4];
+  f32x4a u, v;
+};
+template <> struct Quad<true> {
+  float x[4], g[4];
+  uint32_t cu, cv;
+  int eu, ev;
+};
+
+template <bool WBF, bool Q8, bool WHOLE>
+__device__ __forceinline__ void load_step(Quad<Q8>& q, const void* w, const void* g, uint8_t kind, const RowsOf& rows, const AdamwState& st, const AdamwTensor& t,
+                                          int64_t row0, int64_t col0, int64_t base, int64_t ahead) {
+  const int64_t i = base + ahead, at = t.off + i;
+  const int cnt = WHOLE || t.n - i >= 4 ? 4 : t.n > i ? (int)(t.n - i) : 0;
 #pragma unroll
-  for (int rep = 0; rep < (int)(ADAMW_CHUNK / 1024); ++rep) {
-    const int64_t ahead = rep * 1024 + (int64_t)threadIdx.x * 4, i = base + ahead;
-    if (base + rep * 1024 >= t.n) break;             // uniform
-    const int cnt = t.n - i >= 4 ? 4 : t.n > i ? (int)(t.n - i) : 0;
-    float x[4] = {0.f, 0.f, 0.f, 0.f}, gr[4], u[4], v[4];
-    if (cnt == 4) load_quad<WBF, true>(w, i, x);
-    else
-      for (int e = 0; e < cnt; ++e) x[e] = load_element<WBF>(w, i + e);
-    if constexpr (!Q8) {
-      if (cnt == 0) continue;
-      const f32x4a ou = __builtin_nontemporal_load(reinterpret_cast<const f32x4a*>(a.st.u + t.off + i));     // (the state is padded to whole blocks)
-      const f32x4a ov = __builtin_nontemporal_load(reinterpret_cast<const f32x4a*>(a.st.v + t.off + i));
-      load_gradient(g, index, slots, g_bf16, t.cols, row0, col0, i, ahead, cnt, gr);
+  for (int e = 0; e < 4; ++e) q.x[e] = q.g[e] = 0.f;
+  if constexpr (Q8) { q.cu = q.cv = 0; q.eu = q.ev = 0; }
+  else q.u = q.v = f32x4a{0.f, 0.f, 0.f, 0.f};
+  if (cnt == 0) return;
+  if constexpr (Q8) {
+    q.cu = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(st.cu + at));
+    q.cv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(st.cv + at));
+    q.eu = st.eu[at / Q8_BLOCK];
+    q.ev = st.ev[at / Q8_BLOCK];
+  } else {                                             // (the state is padded to whole blocks)
+    q.u = __builtin_nontemporal_load(reinterpret_cast<const f32x4a*>(st.u + at));
+    q.v = __builtin_nontemporal_load(reinterpret_cast<const f32x4a*>(st.v + at));
+  }
+  if (cnt == 4) load_quad<WBF, true>(w, i, q.x);
+  else
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float s = scale * gr[e];
-        u[e] = fmaf(a.b1, ou[e], a.omb1 * s);
-        v[e] = fmaf(a.b2, ov[e], a.omb2 * s * s);
-      }
-      const f32x4a nu = {u[0], u[1], u[2], u[3]}, nv = {v[0], v[1], v[2], v[3]};
-      __builtin_nontemporal_store(nu, reinterpret_cast<f32x4a*>(a.st.u + t.off + i));
-      __builtin_nontemporal_store(nv, reinterpret_cast<f32x4a*>(a.st.v + t.off + i));
-    } else {
-      // every product and sum is rounded by itself, so that codes do not depend on which of them a compiler joins
-#pragma clang fp contract(off)
-      const int64_t at = t.off + i;
-      const bool any = cnt > 0;
-      uint32_t cu = 0, cv = 0;
-      int eu = 0, ev = 0;
-      if (any) {
-        cu = *reinterpret_cast<const uint32_t*>(a.st.cu + at);
-        cv = *reinterpret_cast<const uint32_t*>(a.st.cv + at);
-        eu = a.st.eu[at / Q8_BLOCK];
-        ev = a.st.ev[at / Q8_BLOCK];
-      }
-      load_gradient(g, index, slots, g_bf16, t.cols, row0, col0, i, ahead, cnt, gr);
-      double du[4], dv[4];
-      uint32_t mix[4];
+    for (int e = 0; e < 4; ++e)
+      if (e < cnt) q.x[e] = load_element<WBF>(w, i + e);
+  const bool bf16 = kind & G_BF16;
+  if (kind & G_ROWS) {
+    load_rows(g, rows, bf16, t.cols, row0, col0, ahead, cnt, q.g);
+  } else if (cnt == 4) {
+    if (bf16) load_quad<true, true>(g, i, q.g);
+    else load_quad<false, true>(g, i, q.g);
+  } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int bu = (cu >> (8 * e)) & 0x7f, bv = (cv >> (8 * e)) & 0xff;
-        const double s = scale_d * (double)gr[e];
-        double ou = q8_value(bu, 127, eu);
-        if ((cu >> (8 * e)) & 0x80) ou = -ou;
-        const double ov = q8_value(bv, 255, ev);
-        const double pu = a.b1d * ou, qu = a.omb1d * s, s2 = s * s, pv = a.b2d * ov, qv = a.omb2d * s2;
-        du[e] = e < cnt ? pu + qu : 0.0;
-        dv[e] = e < cnt ? pv + qv : 0.0;
-        u[e] = (float)du[e]; v[e] = (float)dv[e];
-        mix[e] = q8_mix(turn, (uint32_t)(i + e));
-      }
-      q8_store<false>(a.st, at, any, du, dv, mix);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float den = sqrtf(v[e] * inv_c2) + a.eps;
-      const float n = den == 0.f ? 0.f : u[e] * inv_c1 / den;        // den = 0: eps = 0 and no gradient so far
-      x[e] = fmaf(-a.lr, fmaf(wd, x[e], n), x[e]);
-    }
-    if (cnt == 4) store_quad<WBF, true>(w, i, x);
-    else
-      for (int e = 0; e < cnt; ++e) store_element<WBF>(w, i + e, x[e]);
+    for (int e = 0; e < 4; ++e)
+      if (e < cnt) q.g[e] = bf16 ? load_element<true>(g, i + e) : load_element<false>(g, i + e);
   }
 }
 
-__global__ void k_adamw_advance(StepDev* sd, const float* coef, int32_t* flag) {
-  if (coef && !(fabsf(*coef) < INFINITY)) *flag = 1;
-  else step_write(sd, sd->t + 1);
+static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
+
+struct StepScalars {
+  float scale, inv_c1, inv_c2, wd;
+  double scale_d;
+  uint32_t turn;
+};
+template <bool WBF, bool Q8, bool WHOLE>
+__device__ __forceinline__ void store_step(Quad<Q8>& q, void* w, const AdamwArgs& a, const AdamwTensor& t, const StepScalars& s, int64_t base, int64_t ahead) {
+  const int64_t i = base + ahead, at = t.off + i;
+  const int cnt = WHOLE || t.n - i >= 4 ? 4 : t.n > i ? (int)(t.n - i) : 0;
+  float u[4], v[4];
+  if constexpr (!Q8) {
+    if (cnt == 0) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float g = s.scale * q.g[e];
+      u[e] = fmaf(a.b1, q.u[e], a.omb1 * g);
+      v[e] = fmaf(a.b2, q.v[e], a.omb2 * g * g);
+    }
+    const f32x4a nu = {u[0], u[1], u[2], u[3]}, nv = {v[0], v[1], v[2], v[3]};
+    __builtin_nontemporal_store(nu, reinterpret_cast<f32x4a*>(a.st.u + at));
+    __builtin_nontemporal_store(nv, reinterpret_cast<f32x4a*>(a.st.v + at));
+  } else {
+    // every product and sum is rounded by itself, so that codes do not depend on which of them a compiler joins
+#pragma clang fp contract(off)
+    double du[4], dv[4];
+    uint32_t mix[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int bu = (q.cu >> (8 * e)) & 0x7f, bv = (q.cv >> (8 * e)) & 0xff;
+      const double g = s.scale_d * (double)q.g[e];
+      double ou = q8_value(bu, 127, q.eu);
+      if ((q.cu >> (8 * e)) & 0x80) ou = -ou;
+      const double ov = q8_value(bv, 255, q.ev);
+      const double pu = a.b1d * ou, qu = a.omb1d * g, g2 = g * g, pv = a.b2d * ov, qv = a.omb2d * g2;
+      du[e] = WHOLE || e < cnt ? pu + qu : 0.0;
+      dv[e] = WHOLE || e < cnt ? pv + qv : 0.0;
+      u[e] = (float)du[e]; v[e] = (float)dv[e];
+      mix[e] = q8_mix(s.turn, (uint32_t)(i + e));
+    }
+    q8_store<false>(a.st, at, cnt > 0, du, dv, mix);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float den = sqrtf(v[e] * s.inv_c2) + a.eps;
+    const float n = den == 0.f ? 0.f : u[e] * s.inv_c1 / den;        // den = 0: eps = 0 and no gradient so far
+    q.x[e] = fmaf(-a.lr, fmaf(s.wd, q.x[e], n), q.x[e]);
+  }
+  if (cnt == 4) store_quad<WBF, true>(w, i, q.x);
+  else
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < cnt) store_element<WBF>(w, i + e, q.x[e]);
+}
+
+// The workgroup that is the last of its launch to come here.  Counters for a sixteenth of the workgroups each, so that few wait for one address; the last of each
+// counts on the one behind them, and every counter is left at zero.
+__device__ __forceinline__ bool last_workgroup(int32_t* counters) {
+  const int32_t k = (int32_t)blockIdx.x % COUNTERS, all = ((int32_t)gridDim.x - k + COUNTERS - 1) / COUNTERS;
+  if (atomicAdd(counters + 32 * k, 1) != all - 1) return false;
+  atomicExch(counters + 32 * k, 0);
+  const int32_t used = (int32_t)gridDim.x < COUNTERS ? (int32_t)gridDim.x : COUNTERS;
+  if (atomicAdd(counters + 32 * COUNTERS, 1) != used - 1) return false;
+  atomicExch(counters + 32 * COUNTERS, 0);
+  return true;
+}
+
+constexpr int REPS = (int)(ADAMW_CHUNK / 1024), AHEAD = 2;      // quads of a thread, and how many of them are requested together
+template <bool WBF, bool Q8>
+__global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
+  const int32_t c = a.first[0] + (int32_t)blockIdx.x;
+  const int k = find_tensor(a.first, a.count, c);
+  const AdamwTensor t = a.tensors[k];
+  const float coef = a.coef ? *a.coef : 1.f;
+  if (!(fabsf(coef) < INFINITY)) {                     // the norm was not finite: this step is left out
+    if (a.advance && blockIdx.x == 0 && threadIdx.x == 0) *a.flag = 1;
+    return;
+  }
+  StepScalars s;
+  s.scale_d = a.scale * (double)coef;
+  s.scale = (float)s.scale_d;
+  s.inv_c1 = a.step->next_inv_c1; s.inv_c2 = a.step->next_inv_c2;
+  s.wd = t.decay ? a.wd : 0.f;
+  const int64_t steps = a.step->t;
+  s.turn = (uint32_t)(steps + 1) * STEP_TURN;
+  const int64_t base = (int64_t)(c - a.first[k]) * ADAMW_CHUNK;
+  void* const w = a.w[k];
+  const void* const g = a.g[k];
+  const uint8_t kind = a.kind[k];
+  RowsOf rows{};
+  int64_t row0 = 0, col0 = 0;
+  if (kind & G_ROWS) {
+    rows = a.rows[kind >> 2];
+    row0 = base / t.cols; col0 = base - row0 * t.cols;
+  }
+  if (base + ADAMW_CHUNK <= t.n) {
+#pragma unroll
+    for (int rep = 0; rep < REPS; rep += AHEAD) {
+      Quad<Q8> q[AHEAD];
+#pragma unroll
+      for (int r = 0; r < AHEAD; ++r) load_step<WBF, Q8, true>(q[r], w, g, kind, rows, a.st, t, row0, col0, base, (rep + r) * 1024 + (int64_t)threadIdx.x * 4);
+#pragma unroll
+      for (int r = 0; r < AHEAD; ++r) store_step<WBF, Q8, true>(q[r], w, a, t, s, base, (rep + r) * 1024 + (int64_t)threadIdx.x * 4);
+    }
+  } else {
+    for (int rep = 0; rep < REPS && base + rep * 1024 < t.n; ++rep) {
+      Quad<Q8> q;
+      load_step<WBF, Q8, false>(q, w, g, kind, rows, a.st, t, row0, col0, base, rep * 1024 + (int64_t)threadIdx.x * 4);
+      store_step<WBF, Q8, false>(q, w, a, t, s, base, rep * 1024 + (int64_t)threadIdx.x * 4);
+    }
+  }
+  if (!a.advance) return;
+  // t <- t + 1, once every workgroup has read what belongs to t
+  __syncthreads();
+  if (threadIdx.x == 0 && last_workgroup(a.flag + 32)) step_write(a.step, steps + 1);
 }
 
 // TO_STATE: moments <- [u | v], in 8 bits with thresholds of one half (a value of the grid stays itself); else [u | v] <- moments.  What lies
@@ -307,70 +383,128 @@ __global__ __launch_bounds__(256) void k_moments(AdamwState st, const AdamwTenso
 // products and sums are in double, in an order that the sizes alone fix (each thread's elements, the lanes of a wave, the waves, the workgroups).
 // ---------------------------------------------------------------------------------------
 struct NormArgs {
-  const void* g[NORM_GROUP];
-  const int32_t* owner[NORM_GROUP];      // of rows: the row of the vocabulary that a row of g belongs to, or -1 (null: g is dense)
-  int64_t n[NORM_GROUP], cols[NORM_GROUP];
-  int32_t first[NORM_GROUP];
-  uint8_t bf16[NORM_GROUP];
+  const void* g[GROUP];
+  int32_t first[GROUP];                   // chunks before each
+  uint16_t missing[GROUP];                // elements that its last chunk lacks
+  uint8_t kind[GROUP];
+  RowsOf rows[GROUP_ROWS];
+  int64_t rows_cols[GROUP_ROWS], rows_of[GROUP_ROWS];
   int32_t count, chunks, add;
+  double max_norm;
   double* part;
+  float* out;                             // one workgroup is all: it writes the result itself
 };
+
+static_assert(sizeof(NormArgs) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ double wave_sum(double x) {
   for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
   return x;
 }
-
-__global__ __launch_bounds__(256) void k_norm_part(NormArgs a) {
-  __shared__ double sums[4];
-  double sum = 0.0;
-  for (int32_t c = (int32_t)blockIdx.x; c < a.chunks; c += (int32_t)gridDim.x) {
-    const int k = __builtin_amdgcn_readfirstlane(find_tensor(a.first, a.count, c));
-    const void* const g = a.g[k];
-    const int32_t* const owner = a.owner[k];
-    const int64_t n = a.n[k], base = (int64_t)(c - a.first[k]) * NORM_CHUNK, cols = a.cols[k];
-    const bool bf16 = a.bf16[k] != 0;
-    for (int rep = 0; rep < (int)(NORM_CHUNK / 1024); ++rep) {
-      const int64_t i = base + rep * 1024 + (int64_t)threadIdx.x * 4;
-      if (i >= n) break;
-      const int cnt = n - i >= 4 ? 4 : (int)(n - i);
-      float x[4] = {0.f, 0.f, 0.f, 0.f};
-      if (owner == nullptr || (owner[i / cols] >= 0 && i % cols + cnt <= cols)) {
-        if (cnt == 4) {
-          if (bf16) load_quad<true, true>(g, i, x);
-          else load_quad<false, true>(g, i, x);
-        } else {
-          for (int e = 0; e < cnt; ++e) x[e] = bf16 ? load_element<true>(g, i + e) : load_element<false>(g, i + e);
-        }
-      } else {
-        for (int e = 0; e < cnt; ++e)
-          if (owner[(i + e) / cols] >= 0) x[e] = bf16 ? load_element<true>(g, i + e) : load_element<false>(g, i + e);
-      }
-      for (int e = 0; e < 4; ++e) sum = fma((double)x[e], (double)x[e], sum);
-    }
-  }
-  sum = wave_sum(sum);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+// The sum over the threads of a workgroup, in thread 0.
+__device__ __forceinline__ double block_sum(double x, double* sums) {
+  x = wave_sum(x);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = x;
   __syncthreads();
   if (threadIdx.x == 0) {
-    sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    a.part[blockIdx.x] = a.add ? a.part[blockIdx.x] + sum : sum;
+    x = 0.0;
+    for (int k = 0; k < (int)blockDim.x / 64; ++k) x += sums[k];
   }
+  return x;
+}
+__device__ __forceinline__ void norm_result(double sum, double max_norm, float* out) {
+  const double norm = sqrt(sum);
+  out[0] = (float)norm;
+  out[1] = !(norm < (double)INFINITY) ? __uint_as_float(0x7fc00000u) : norm > max_norm ? (float)(max_norm / norm) : 1.f;
 }
 
-__global__ __launch_bounds__(1024) void k_norm_sum(const double* part, int32_t count, double max_norm, float* out) {
-  __shared__ double sums[16];
-  double sum = (int)threadIdx.x < count ? part[threadIdx.x] : 0.0;
-  sum = wave_sum(sum);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    sum = 0.0;
-    for (int k = 0; k < 16; ++k) sum += sums[k];
-    const double norm = sqrt(sum);
-    out[0] = (float)norm;
-    out[1] = !(norm < (double)INFINITY) ? __uint_as_float(0x7fc00000u) : norm > max_norm ? (float)(max_norm / norm) : 1.f;
+// Squares of a chunk, sixteen bytes a thread at a time.
+template <bool BF>
+__device__ __forceinline__ double chunk_squares(const void* g, int64_t base, int64_t n, int threads) {
+  constexpr int VEC = BF ? 8 : 4, AHEAD = 4;
+  double sum[2] = {0.0, 0.0};
+  const int64_t end = std::min(base + NORM_CHUNK, n), step = (int64_t)threads * VEC;
+  int64_t i = base + (int64_t)threadIdx.x * VEC;
+  for (; i + (AHEAD - 1) * step + VEC <= end; i += AHEAD * step) {
+    Piece<BF, VEC> p[AHEAD];
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) p[q].load(g, i + q * step);
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum[e & 1] = fma((double)p[q].value(e), (double)p[q].value(e), sum[e & 1]);
   }
+  for (; i < end; i += step)
+    for (int e = 0; e < VEC && i + e < end; ++e) {
+      const double x = (double)load_element<BF>(g, i + e);
+      sum[e & 1] = fma(x, x, sum[e & 1]);
+    }
+  return sum[0] + sum[1];
+}
+// The same of a gradient by rows: rows that belong to no row of the tensor hold nothing.
+template <bool BF>
+__device__ __forceinline__ double chunk_squares_of_rows(const void* g, const int32_t* owner, int64_t cols, int64_t base, int64_t n, int threads) {
+  double sum = 0.0;
+  const int64_t end = std::min(base + NORM_CHUNK, n), row0 = base / cols, col0 = base - row0 * cols;
+  for (int64_t i = base + (int64_t)threadIdx.x * 4; i < end; i += (int64_t)threads * 4) {
+    const uint64_t c = (uint64_t)(col0 + (i - base));
+    int64_t row, col;
+    if (cols < (int64_t(1) << 31)) {
+      const uint32_t q = (uint32_t)c / (uint32_t)cols;
+      row = row0 + q; col = (int64_t)((uint32_t)c - q * (uint32_t)cols);
+    } else {
+      row = row0 + (int64_t)(c / (uint64_t)cols); col = (int64_t)(c % (uint64_t)cols);
+    }
+    if (i + 4 <= end && col + 4 <= cols) {
+      if (owner[row] < 0) continue;
+      float x[4];
+      load_quad<BF, false>(g, i, x);
+      for (int e = 0; e < 4; ++e) sum = fma((double)x[e], (double)x[e], sum);
+    } else {
+      for (int e = 0; e < 4 && i + e < end; ++e) {
+        if (owner[row] >= 0) {
+          const double x = (double)load_element<BF>(g, i + e);
+          sum = fma(x, x, sum);
+        }
+        if (++col == cols) { col = 0; ++row; }
+      }
+    }
+  }
+  return sum;
+}
+
+__global__ __launch_bounds__(1024) void k_norm_part(NormArgs a) {
+  __shared__ double sums[16];
+  double sum = 0.0;
+  const int threads = (int)blockDim.x;
+  int k = find_tensor(a.first, a.count, (int32_t)blockIdx.x);
+  for (int32_t c = (int32_t)blockIdx.x; c < a.chunks; c += (int32_t)gridDim.x) {
+    while (k + 1 < a.count && a.first[k + 1] <= c) ++k;
+    const int32_t chunks = (k + 1 < a.count ? a.first[k + 1] : a.chunks) - a.first[k];
+    const int64_t n = (int64_t)chunks * NORM_CHUNK - a.missing[k], base = (int64_t)(c - a.first[k]) * NORM_CHUNK;
+    const uint8_t kind = a.kind[k];
+    if (kind & G_ROWS) {
+      const int r = kind >> 2;
+      const int32_t* owner = a.rows[r].index + a.rows_of[r];
+      sum += kind & G_BF16 ? chunk_squares_of_rows<true>(a.g[k], owner, a.rows_cols[r], base, n, threads)
+                           : chunk_squares_of_rows<false>(a.g[k], owner, a.rows_cols[r], base, n, threads);
+    } else {
+      sum += kind & G_BF16 ? chunk_squares<true>(a.g[k], base, n, threads) : chunk_squares<false>(a.g[k], base, n, threads);
+    }
+  }
+  sum = block_sum(sum, sums);
+  if (threadIdx.x != 0) return;
+  if (a.out) norm_result(sum, a.max_norm, a.out);
+  else a.part[blockIdx.x] = a.add ? a.part[blockIdx.x] + sum : sum;
+}
+
+__global__ __launch_bounds__(256) void k_norm_sum(const double* part, int32_t count, double max_norm, float* out) {
+  __shared__ double sums[4];
+  double sum = 0.0;
+#pragma unroll
+  for (int q = 0; q < NORM_BLOCKS / 256; ++q) sum += (int)threadIdx.x + 256 * q < count ? part[threadIdx.x + 256 * q] : 0.0;
+  sum = block_sum(sum, sums);
+  if (threadIdx.x == 0) norm_result(sum, max_norm, out);
 }
 
 }  // namespace lordo
@@ -439,7 +573,7 @@ int plan_adamw(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams
   c.shapes.assign(tensors, tensors + n);
   int64_t at = 0;
   auto take = [&](int64_t bytes) { const int64_t r = at; at += (bytes + 255) & ~int64_t(255); return r; };
-  c.flag = take(256);
+  c.flag = take(128 + 128 * (COUNTERS + 1));
   c.step = take(sizeof(StepDev));
   c.table = take((int64_t)sizeof(AdamwTensor) * n);
   c.prefix = take((int64_t)sizeof(int32_t) * (n + 1));
@@ -464,6 +598,8 @@ bool good_grad(const lordo_grad& g) {
   }
   return (reinterpret_cast<uintptr_t>(g.data) & (g.dtype == LORDO_F32 ? 3 : 1)) == 0 && (reinterpret_cast<uintptr_t>(g.index) & 3) == 0;
 }
+
+uint8_t grad_kind(const lordo_grad& g, int rows) { return (uint8_t)((g.dtype == LORDO_BF16 ? G_BF16 : 0) | (g.index ? G_ROWS | rows << 2 : 0)); }
 
 #define ADAMW_CHK(expr, what)                                                                     \
   do {                                                                                            \
@@ -524,7 +660,7 @@ int lordo_adamw_init(lordo_adamw** out, const lordo_tensor* tensors, int32_t n, 
     ADAMW_CHK(hipStreamSynchronize(s), "hipStreamSynchronize");
     ADAMW_CHK(hipMemcpy(c->arena + c->table, c->tensors.data(), sizeof(AdamwTensor) * n, hipMemcpyHostToDevice), "hipMemcpy");
     ADAMW_CHK(hipMemcpy(c->arena + c->prefix, c->first.data(), sizeof(int32_t) * (n + 1), hipMemcpyHostToDevice), "hipMemcpy");
-    ADAMW_CHK(launch_fill_zero(c->arena + c->flag, 256, s), "fill");
+    ADAMW_CHK(launch_fill_zero(c->arena + c->flag, c->step - c->flag, s), "fill");
     ADAMW_CHK(launch_fill_zero(c->arena + c->u, (int64_t)c->bytes - c->u, s), "fill");
     ADAMW_CHK(launch_step_set(c->step_dev(), hp->beta1, hp->beta2, hp->bias_correction, 0, s), "k_step_set");
     ADAMW_CHK(hipStreamSynchronize(s), "hipStreamSynchronize");
@@ -558,18 +694,22 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
   a.coef = coef;
   a.step = c->step_dev();
   a.st = c->state();
-  for (int at = 0; at < n; at += ADAMW_GROUP) {
-    a.count = std::min(ADAMW_GROUP, n - at);
-    for (int k = 0; k < a.count; ++k) {
-      a.w[k] = W[at + k];
-      a.g[k] = G[at + k].data;
-      a.index[k] = G[at + k].index;
-      a.slots[k] = (int32_t)G[at + k].slots;
-      a.g_bf16[k] = G[at + k].dtype == LORDO_BF16;
+  a.flag = reinterpret_cast<int32_t*>(c->arena + c->flag);
+  for (int at = 0; at < n;) {
+    a.count = 0;
+    for (int rows = 0; at + a.count < n && a.count < GROUP; ++a.count) {
+      const lordo_grad& g = G[at + a.count];
+      if (g.index && rows == GROUP_ROWS) break;
+      a.w[a.count] = W[at + a.count];
+      a.g[a.count] = g.data;
+      a.kind[a.count] = grad_kind(g, rows);
+      if (g.index) a.rows[rows++] = RowsOf{g.index, (int32_t)g.slots};
     }
     a.tensors = reinterpret_cast<const AdamwTensor*>(c->arena + c->table) + at;
     a.first = reinterpret_cast<const int32_t*>(c->arena + c->prefix) + at;
     const dim3 grid((unsigned)(c->first[at + a.count] - c->first[at])), block(256);
+    at += a.count;
+    a.advance = at == n;
     const bool bf = c->hp.param_dtype == LORDO_BF16;
     if (c->hp.state_dtype == LORDO_Q8) {
       if (bf) hipLaunchKernelGGL((k_adamw<true, true>), grid, block, 0, s, a);
@@ -581,9 +721,6 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
     const int rc = launched("k_adamw");
     if (rc != LORDO_OK) return rc;
   }
-  hipLaunchKernelGGL(k_adamw_advance, dim3(1), dim3(1), 0, s, c->step_dev(), coef, reinterpret_cast<int32_t*>(c->arena + c->flag));
-  const int rc = launched("k_adamw_advance");
-  if (rc != LORDO_OK) return rc;
   ++c->t;
   c->step_dirty = false;
   return LORDO_OK;
@@ -629,7 +766,7 @@ int lordo_adamw_poll_status(lordo_adamw* c, void* stream) {
   int32_t flag = 0;
   ADAMW_CHK(hipMemcpy(&flag, c->arena + c->flag, sizeof(flag), hipMemcpyDeviceToHost), "hipMemcpy");
   if (flag == 0) return LORDO_OK;
-  ADAMW_CHK(launch_fill_zero(c->arena + c->flag, 256, s), "fill");
+  ADAMW_CHK(launch_fill_zero(c->arena + c->flag, 16, s), "fill");
   ADAMW_CHK(hipStreamSynchronize(s), "hipStreamSynchronize");
   return LORDO_ENUMERIC;
 }
@@ -641,39 +778,49 @@ int lordo_grad_norm(const lordo_grad* G, int32_t n, double max_norm, float* out,
   if ((reinterpret_cast<uintptr_t>(out) & 3) != 0 || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return LORDO_EINVAL;
   if (workspace_bytes < LORDO_NORM_WORKSPACE_BYTES) return LORDO_ENOMEM;
   auto elements = [](const lordo_grad& g) { return g.index ? g.slots * g.cols : g.rows * g.cols; };
-  int64_t most = 1;
-  for (int at = 0; at < n; at += NORM_GROUP) {
-    int64_t chunks = 0;
-    for (int i = at; i < std::min(n, at + NORM_GROUP); ++i) {
-      if (!good_grad(G[i])) return LORDO_EINVAL;
-      chunks += (elements(G[i]) + NORM_CHUNK - 1) / NORM_CHUNK;
-    }
-    if (chunks > (int64_t(1) << 30)) return LORDO_EINVAL;
-    most = std::max(most, chunks);
+  int64_t all = 0;
+  for (int i = 0; i < n; ++i) {
+    if (!good_grad(G[i])) return LORDO_EINVAL;
+    all += (elements(G[i]) + NORM_CHUNK - 1) / NORM_CHUNK;
+    if (all > (int64_t(1) << 30)) return LORDO_EINVAL;
   }
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const int blocks = (int)std::min<int64_t>(most, NORM_BLOCKS);      // the same for every launch: each adds to the sums of the one before
+  const int blocks = (int)std::min<int64_t>(std::max<int64_t>(all, 1), NORM_BLOCKS);      // of every launch: each adds to the sums of the one before
+  const bool one = n <= GROUP && all <= NORM_ALONE;
   NormArgs a;
   a.part = reinterpret_cast<double*>(workspace);
-  for (int at = 0; at < n; at += NORM_GROUP) {
-    a.count = std::min(NORM_GROUP, n - at);
+  a.max_norm = max_norm;
+  a.out = nullptr;
+  for (int at = 0; at < n;) {
+    a.count = 0;
     a.chunks = 0;
-    for (int k = 0; k < a.count; ++k) {
-      const lordo_grad& g = G[at + k];
-      a.g[k] = g.data;
-      a.owner[k] = g.index ? g.index + g.rows : nullptr;
-      a.n[k] = elements(g);
-      a.cols[k] = g.cols;
-      a.bf16[k] = g.dtype == LORDO_BF16;
-      a.first[k] = a.chunks;
-      a.chunks += (int32_t)((a.n[k] + NORM_CHUNK - 1) / NORM_CHUNK);
-    }
     a.add = at > 0;
+    for (int rows = 0; at + a.count < n && a.count < GROUP; ++a.count) {
+      const lordo_grad& g = G[at + a.count];
+      if (g.index && rows == GROUP_ROWS) break;
+      const int64_t m = elements(g), chunks = (m + NORM_CHUNK - 1) / NORM_CHUNK;
+      a.g[a.count] = g.data;
+      a.first[a.count] = a.chunks;
+      a.missing[a.count] = (uint16_t)(chunks * NORM_CHUNK - m);
+      a.kind[a.count] = grad_kind(g, rows);
+      if (g.index) {
+        a.rows[rows] = RowsOf{g.index, (int32_t)g.slots};
+        a.rows_cols[rows] = g.cols;
+        a.rows_of[rows++] = g.rows;
+      }
+      a.chunks += (int32_t)chunks;
+    }
+    at += a.count;
+    if (one && at == n && !a.add) {
+      a.out = out;
+      hipLaunchKernelGGL(k_norm_part, dim3(1), dim3(1024), 0, s, a);
+      return launched("k_norm_part");
+    }
     hipLaunchKernelGGL(k_norm_part, dim3((unsigned)blocks), dim3(256), 0, s, a);
     const int rc = launched("k_norm_part");
     if (rc != LORDO_OK) return rc;
   }
-  hipLaunchKernelGGL(k_norm_sum, dim3(1), dim3(1024), 0, s, a.part, blocks, max_norm, out);
+  hipLaunchKernelGGL(k_norm_sum, dim3(1), dim3(256), 0, s, a.part, blocks, max_norm, out);
   return launched("k_norm_sum");
 }
 
