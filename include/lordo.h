@@ -367,7 +367,7 @@ typedef struct {
 } lordo_grad;
 
 typedef struct {
-  double  beta1, beta2, eps;     /* as in lordo_hparams: in [0, 1), eps >= 0 outside the root */
+  double  beta1, beta2, eps;     /* as in lordo_hparams: in [0, 1), eps outside the root, 0 or from 2^-126 on */
   double  weight_decay;          /* decoupled: W <- W - lr * weight_decay * W, >= 0 */
   int32_t bias_correction;       /* as in lordo_hparams */
   int32_t param_dtype;           /* LORDO_F32 or LORDO_BF16 storage of every W (formed in fp32, rounded to nearest-even once) */
@@ -378,7 +378,7 @@ typedef struct {
                                     w / 2^17, w the upper 17 bits of x for u and the lower 17 for v, in 32 bits x = t 0x9E3779B1 + i 0xBB67AE85 for element
                                     i of its tensor at step t; x = (x xor x>>15) 0x6A09E667; x = x xor x>>14.  So it rounds up in the right share of
                                     the steps, and changes below the grid (1 - beta2 of v a step) add up.
-                                    v > 0 is never held as 0; u below its least value takes it by the same rule, or 0.  W is updated from the moments before this rounding.  An infinity, a NaN or more than 2^127
+                                    v > 0 is never held as 0 (unless its block is 0 in fp32); u below its least value takes it by the same rule, or 0.  W is updated from the moments before this rounding.  An infinity, a NaN or more than 2^127
                                     makes the moments of its whole block NaN */
   int32_t reserved;              /* must be 0 */
 } lordo_adamw_hparams;

@@ -18,11 +18,12 @@ typedef float f32x4a __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4a __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float bf16_value(uint32_t h) { return __uint_as_float(h << 16); }
-// nearest-even; a NaN stays a quiet one
-__device__ __forceinline__ uint32_t bf16_bits(float x) {
-  const uint32_t u = __float_as_uint(x);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;
-  return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {      // the conversion instruction: two at once, nearest-even
+  const f32x2 x = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
 }
 
 template <bool BF>
@@ -32,7 +33,7 @@ __device__ __forceinline__ float load_element(const void* p, int64_t i) {
 }
 template <bool BF>
 __device__ __forceinline__ void store_element(void* p, int64_t i, float x) {
-  if constexpr (BF) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)bf16_bits(x);
+  if constexpr (BF) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)bf16_pair(x, 0.f);
   else reinterpret_cast<float*>(p)[i] = x;
 }
 // STREAM: touched once a call, by one workgroup: kept out of the caches' way
@@ -56,9 +57,7 @@ __device__ __forceinline__ void load_quad(const void* p, int64_t i, float (&x)[4
 template <bool BF, bool STREAM>
 __device__ __forceinline__ void store_quad(void* p, int64_t i, const float (&x)[4]) {
   if constexpr (BF) {
-    u32x2u t;
-    t.x = bf16_bits(x[0]) | bf16_bits(x[1]) << 16;
-    t.y = bf16_bits(x[2]) | bf16_bits(x[3]) << 16;
+    const u32x2u t = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
     u32x2u* q = reinterpret_cast<u32x2u*>(reinterpret_cast<uint16_t*>(p) + i);
     if constexpr (STREAM) __builtin_nontemporal_store(t, q);
     else *q = t;

@@ -67,31 +67,24 @@ struct AdamwArgs {
 // of 4096 elements is within 1 % of beta^2000.  (Turning w by a fixed fraction from step to step instead was 17 % low: which steps round up then
 // depends on the step before.)
 // ---------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t q8_mix(uint32_t of_step, uint32_t element) {       // of_step: t times the first constant
-  uint32_t x = of_step + element * 0xBB67AE85u;
+constexpr uint32_t Q8_STEP = 0x9E3779B1u, Q8_ELEMENT = 0xBB67AE85u;
+__device__ __forceinline__ uint32_t q8_mix(uint32_t x) {       // x = step Q8_STEP + element Q8_ELEMENT
   x = (x ^ (x >> 15)) * 0x6A09E667u;
   return x ^ (x >> 14);
 }
-constexpr uint32_t STEP_TURN = 0x9E3779B1u;
-constexpr uint32_t Q8_HALF = 1u << 16;
 constexpr int Q8_NAN = 255;              // exponent of a block that holds an infinity or a NaN (or more than 2^127): all its values are NaN
 
-// `exponent` is biased as in fp32; code without sign, top = 127 or 255
-__device__ __forceinline__ double q8_value(int code, int top, int exponent) {
-  if (exponent == Q8_NAN) return __longlong_as_double(0x7ff8000000000000ll);
-  return code == 0 ? 0.0 : __hiloint2double((code - top + 8 * (exponent + 1023 - 127)) << 17, 0);
-}
+// Four codes of a thread -> moments (not NaN ones: the callers see to those by the exponent).
 template <bool SIGNED>
-__device__ __forceinline__ uint32_t q8_code(double x, int exponent, uint32_t w) {
-  constexpr int TOP = SIGNED ? 127 : 255;
-  constexpr double LEAST = SIGNED ? 1.25 / 65536.0 : 1.25 / 4294967296.0;
-  const double m = fabs(x);
-  int code = min((int)(((uint32_t)__double2hiint(m) + w) >> 17) - 8 * (exponent + 1023 - 127) + TOP, TOP);
-  const double y = m * __hiloint2double((1023 + 127 - exponent) << 20, 0);
-  if (y < LEAST) code = SIGNED ? (int)(((uint32_t)(int)(fmin(y, LEAST) * (131072.0 / LEAST)) + w) >> 17) : 1;
-  if (!(y > 0.0)) code = 0;
-  if constexpr (SIGNED) return (uint32_t)code | (x < 0.0 && code ? 0x80u : 0u);
-  else return (uint32_t)code;
+__device__ __forceinline__ void q8_decode(uint32_t codes, int exponent, double (&x)[4]) {
+  const int top = 8 * (exponent + 1023 - 127) - (SIGNED ? 127 : 255);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int code = (codes >> (8 * e)) & (SIGNED ? 0x7f : 0xff);
+    uint32_t hi = code ? (uint32_t)(code + top) << 17 : 0;
+    if constexpr (SIGNED) hi |= (codes >> (8 * e) & 0x80) << 24;
+    x[e] = __hiloint2double((int)hi, 0);
+  }
 }
 
 // Largest of 32 lanes, by the bits of magnitudes: integers order a NaN above everything, so it is not lost.
@@ -111,34 +104,50 @@ __device__ __forceinline__ uint32_t max32(uint32_t v) {
 // Exponent of the least power of two not below the magnitude with these bits, biased; 0 where all are zero.
 __device__ __forceinline__ int q8_exponent(uint32_t bits) { return bits == 0 ? 0 : (int)min(((bits - 1) >> 23) + 1, (uint32_t)Q8_NAN); }
 
-// Codes of four elements a thread holds (32 lanes a block) from the moments in double; w of u is the upper, of v the lower 17 bits of mix, or 2^16 of both (HALF).
-template <bool HALF>
-__device__ __forceinline__ void q8_store(const AdamwState& st, int64_t at, bool any, const double (&u)[4], const double (&v)[4], const uint32_t (&mix)[4]) {
-  uint32_t mu = 0, mv = 0;
+// Four moments of a thread (32 lanes are a block) -> codes; x32 are the moments in fp32, whose largest sets the exponent; w(e) the thresholds.  A wave
+// with no value of u below the least one, nearly every wave, skips what such values need; v below it takes it whatever the threshold, a maximum.
+template <bool SIGNED, class W>
+__device__ __forceinline__ uint32_t q8_encode(const double (&x)[4], const float (&x32)[4], W w, int& exponent) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(x32[e]) & 0x7fffffffu);
+  exponent = q8_exponent(max32(most));
+  const int top = 8 * (exponent + 1023 - 127) - (SIGNED ? 127 : 255);
+  const uint32_t some = exponent == 0 ? 0 : SIGNED ? 0x7f : 0xff;               // nothing that fp32 holds: zeros
+  int code[4];
+  uint32_t low = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    mu = max(mu, __float_as_uint(fabsf((float)u[e])));
-    mv = max(mv, __float_as_uint(fabsf((float)v[e])));
+    const uint32_t m = (uint32_t)__double2hiint(x[e]) & 0x7fffffffu;
+    code[e] = (int)((m + w(e)) >> 17) - top;
+    if constexpr (!SIGNED) code[e] = max(code[e], 1);
+    code[e] = m ? code[e] : 0;
+    // 1.25 2^-16 of 2^E in the upper half of a double: below it, but not zero
+    if constexpr (SIGNED) low |= (uint32_t)(m - 1 < (((uint32_t)(exponent + 1023 - 127 - 16) << 20) | 2u << 17) - 1);
   }
-  const int eu = q8_exponent(max32(mu)), ev = q8_exponent(max32(mv));
-  uint32_t pu = 0, pv = 0;
+  if constexpr (SIGNED) {
+    if (__any(low)) {
+      constexpr double LEAST = 1.25 / 65536.0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const double y = fabs(x[e]) * __hiloint2double((1023 + 127 - exponent) << 20, 0);
+        if (y < LEAST) code[e] = (int)(((uint32_t)(int)(y * (131072.0 / LEAST)) + w(e)) >> 17);
+      }
+    }
+  }
+  uint32_t codes = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    pu |= q8_code<true>(u[e], eu, HALF ? Q8_HALF : mix[e] >> 15) << (8 * e);
-    pv |= q8_code<false>(v[e], ev, HALF ? Q8_HALF : mix[e] & 0x1ffffu) << (8 * e);
+    uint32_t c = (uint32_t)code[e] & some;
+    if constexpr (SIGNED) c |= ((uint32_t)__double2hiint(x[e]) >> 24) & 0x80u;
+    codes |= c << (8 * e);
   }
-  if (!any) return;
-  *reinterpret_cast<uint32_t*>(st.cu + at) = pu;
-  *reinterpret_cast<uint32_t*>(st.cv + at) = pv;
-  if ((threadIdx.x & 31) == 0) {
-    st.eu[at / Q8_BLOCK] = (uint8_t)eu;
-    st.ev[at / Q8_BLOCK] = (uint8_t)ev;
-  }
+  return codes;
 }
 
-// Gradient of four elements from i on, `cnt` of them there, of a tensor whose gradient is held by rows: i = (row0, col0) + ahead.
-__device__ __forceinline__ void load_rows(const void* g, const RowsOf& rows, bool bf16, int64_t cols, int64_t row0, int64_t col0, int64_t ahead, int cnt,
-                                          float (&x)[4]) {
+// Gradient of four elements, `cnt` of them there, of a tensor whose gradient is held by rows: from (row0, col0) + ahead on.
+template <bool BF16>
+__device__ __forceinline__ void load_rows(const void* g, const RowsOf& rows, int64_t cols, int64_t row0, int64_t col0, uint32_t ahead, int cnt, float (&x)[4]) {
   const uint64_t c = (uint64_t)(col0 + ahead);
   int64_t row, col;
   if (cols < (int64_t(1) << 31)) {                     // then c is below 2^32
@@ -150,8 +159,7 @@ __device__ __forceinline__ void load_rows(const void* g, const RowsOf& rows, boo
   if (cnt == 4 && col + 4 <= cols) {
     const int32_t slot = rows.index[row];
     if ((uint32_t)slot < (uint32_t)rows.slots) {
-      if (bf16) load_quad<true, true>(g, slot * cols + col, x);
-      else load_quad<false, true>(g, slot * cols + col, x);
+      load_quad<BF16, true>(g, slot * cols + col, x);
     }
     return;
   }
@@ -159,7 +167,7 @@ __device__ __forceinline__ void load_rows(const void* g, const RowsOf& rows, boo
   for (int e = 0; e < 4; ++e) {
     if (e >= cnt) break;
     const int32_t slot = rows.index[row];
-    if ((uint32_t)slot < (uint32_t)rows.slots) x[e] = bf16 ? load_element<true>(g, slot * cols + col) : load_element<false>(g, slot * cols + col);
+    if ((uint32_t)slot < (uint32_t)rows.slots) x[e] = load_element<BF16>(g, slot * cols + col);
     if (++col == cols) { col = 0; ++row; }
   }
 }
@@ -175,55 +183,71 @@ template <> struct Quad<true> {
   uint32_t cu, cv;
   int eu, ev;
 };
+// A chunk of a tensor: addresses of its first element, so that a thread adds 32 bits.
+struct Chunk {
+  void* w;
+  const void* g;
+  const RowsOf* rows;
+  float *u, *v;
+  uint8_t *cu, *cv, *eu, *ev;
+  int64_t cols, row0, col0;
+  int32_t n;               // elements there
+  uint32_t element;        // the first, of the tensor (lower 32 bits)
+};
+enum GradKind : int { DENSE_F32 = 0, DENSE_BF16 = G_BF16, ROWS_F32 = G_ROWS, ROWS_BF16 = G_ROWS | G_BF16 };
 
-template <bool WBF, bool Q8, bool WHOLE>
-__device__ __forceinline__ void load_step(Quad<Q8>& q, const void* w, const void* g, uint8_t kind, const RowsOf& rows, const AdamwState& st, const AdamwTensor& t,
-                                          int64_t row0, int64_t col0, int64_t base, int64_t ahead) {
-  const int64_t i = base + ahead, at = t.off + i;
-  const int cnt = WHOLE || t.n - i >= 4 ? 4 : t.n > i ? (int)(t.n - i) : 0;
+template <bool WBF, bool Q8, bool WHOLE, int KIND>
+__device__ __forceinline__ void load_step(Quad<Q8>& q, const Chunk& c, uint32_t i) {
+  constexpr bool BF16 = KIND & G_BF16;
+  const int cnt = WHOLE || c.n - (int)i >= 4 ? 4 : c.n > (int)i ? c.n - (int)i : 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) q.x[e] = q.g[e] = 0.f;
   if constexpr (Q8) { q.cu = q.cv = 0; q.eu = q.ev = 0; }
   else q.u = q.v = f32x4a{0.f, 0.f, 0.f, 0.f};
   if (cnt == 0) return;
   if constexpr (Q8) {
-    q.cu = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(st.cu + at));
-    q.cv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(st.cv + at));
-    q.eu = st.eu[at / Q8_BLOCK];
-    q.ev = st.ev[at / Q8_BLOCK];
+    q.cu = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(c.cu + i));
+    q.cv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(c.cv + i));
+    q.eu = c.eu[i / Q8_BLOCK];
+    q.ev = c.ev[i / Q8_BLOCK];
   } else {                                             // (the state is padded to whole blocks)
-    q.u = __builtin_nontemporal_load(reinterpret_cast<const f32x4a*>(st.u + at));
-    q.v = __builtin_nontemporal_load(reinterpret_cast<const f32x4a*>(st.v + at));
+    q.u = __builtin_nontemporal_load(reinterpret_cast<const f32x4a*>(c.u + i));
+    q.v = __builtin_nontemporal_load(reinterpret_cast<const f32x4a*>(c.v + i));
   }
-  if (cnt == 4) load_quad<WBF, true>(w, i, q.x);
+  if (cnt == 4) load_quad<WBF, true>(c.w, i, q.x);
   else
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (e < cnt) q.x[e] = load_element<WBF>(w, i + e);
-  const bool bf16 = kind & G_BF16;
-  if (kind & G_ROWS) {
-    load_rows(g, rows, bf16, t.cols, row0, col0, ahead, cnt, q.g);
+      if (e < cnt) q.x[e] = load_element<WBF>(c.w, i + e);
+  if constexpr (KIND & G_ROWS) {
+    load_rows<BF16>(c.g, *c.rows, c.cols, c.row0, c.col0, i, cnt, q.g);
   } else if (cnt == 4) {
-    if (bf16) load_quad<true, true>(g, i, q.g);
-    else load_quad<false, true>(g, i, q.g);
+    load_quad<BF16, true>(c.g, i, q.g);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (e < cnt) q.g[e] = bf16 ? load_element<true>(g, i + e) : load_element<false>(g, i + e);
+      if (e < cnt) q.g[e] = load_element<BF16>(c.g, i + e);
   }
 }
 
-static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
-
 struct StepScalars {
   float scale, inv_c1, inv_c2, wd;
-  double scale_d;
+  double omb1_scale, omb2_scale2;      // (1 - beta1) s and (1 - beta2) s^2
   uint32_t turn;
 };
+
+// (u / c1) / (sqrt(v / c2) + eps) by the approximate root and reciprocal (one unit in the last place each): the root's argument is brought out of the
+// subnormal range, which the instruction does not take, and so is no sum with eps in it (the host refuses an eps there).
+__device__ __forceinline__ float update_of(float u, float v, float inv_c1, float inv_c2, float eps) {
+  const float x = v * inv_c2;
+  const bool small = x < 0x1p-96f;
+  const float den = fmaf(__builtin_amdgcn_sqrtf(small ? x * 0x1p64f : x), small ? 0x1p-32f : 1.f, eps);
+  return den == 0.f ? 0.f : u * inv_c1 * __builtin_amdgcn_rcpf(den);       // den = 0: eps = 0 and no gradient so far
+}
+
 template <bool WBF, bool Q8, bool WHOLE>
-__device__ __forceinline__ void store_step(Quad<Q8>& q, void* w, const AdamwArgs& a, const AdamwTensor& t, const StepScalars& s, int64_t base, int64_t ahead) {
-  const int64_t i = base + ahead, at = t.off + i;
-  const int cnt = WHOLE || t.n - i >= 4 ? 4 : t.n > i ? (int)(t.n - i) : 0;
+__device__ __forceinline__ void store_step(Quad<Q8>& q, const AdamwArgs& a, const Chunk& c, const StepScalars& s, uint32_t i) {
+  const int cnt = WHOLE || c.n - (int)i >= 4 ? 4 : c.n > (int)i ? c.n - (int)i : 0;
   float u[4], v[4];
   if constexpr (!Q8) {
     if (cnt == 0) return;
@@ -234,39 +258,45 @@ __device__ __forceinline__ void store_step(Quad<Q8>& q, void* w, const AdamwArgs
       v[e] = fmaf(a.b2, q.v[e], a.omb2 * g * g);
     }
     const f32x4a nu = {u[0], u[1], u[2], u[3]}, nv = {v[0], v[1], v[2], v[3]};
-    __builtin_nontemporal_store(nu, reinterpret_cast<f32x4a*>(a.st.u + at));
-    __builtin_nontemporal_store(nv, reinterpret_cast<f32x4a*>(a.st.v + at));
+    __builtin_nontemporal_store(nu, reinterpret_cast<f32x4a*>(c.u + i));
+    __builtin_nontemporal_store(nv, reinterpret_cast<f32x4a*>(c.v + i));
   } else {
     // every product and sum is rounded by itself, so that codes do not depend on which of them a compiler joins
 #pragma clang fp contract(off)
     double du[4], dv[4];
+    q8_decode<true>(q.cu, q.eu, du);
+    q8_decode<false>(q.cv, q.ev, dv);
+    const double nan = __hiloint2double(0x7ff80000, 0), b1 = q.eu == Q8_NAN ? nan : a.b1d, b2 = q.ev == Q8_NAN ? nan : a.b2d;
+    const uint32_t mix0 = s.turn + (c.element + i) * Q8_ELEMENT;
     uint32_t mix[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int bu = (q.cu >> (8 * e)) & 0x7f, bv = (q.cv >> (8 * e)) & 0xff;
-      const double g = s.scale_d * (double)q.g[e];
-      double ou = q8_value(bu, 127, q.eu);
-      if ((q.cu >> (8 * e)) & 0x80) ou = -ou;
-      const double ov = q8_value(bv, 255, q.ev);
-      const double pu = a.b1d * ou, qu = a.omb1d * g, g2 = g * g, pv = a.b2d * ov, qv = a.omb2d * g2;
+      const double g = (double)q.g[e], g2 = g * g;
+      const double pu = b1 * du[e], qu = s.omb1_scale * g, pv = b2 * dv[e], qv = s.omb2_scale2 * g2;
       du[e] = WHOLE || e < cnt ? pu + qu : 0.0;
       dv[e] = WHOLE || e < cnt ? pv + qv : 0.0;
       u[e] = (float)du[e]; v[e] = (float)dv[e];
-      mix[e] = q8_mix(s.turn, (uint32_t)(i + e));
+      mix[e] = q8_mix(mix0 + e * Q8_ELEMENT);
     }
-    q8_store<false>(a.st, at, cnt > 0, du, dv, mix);
+    int eu, ev;
+    const uint32_t cu = q8_encode<true>(du, u, [&](int e) { return mix[e] >> 15; }, eu);
+    const uint32_t cv = q8_encode<false>(dv, v, [&](int e) { return mix[e] & 0x1ffffu; }, ev);
+    if (cnt > 0) {
+      __builtin_nontemporal_store(cu, reinterpret_cast<uint32_t*>(c.cu + i));
+      __builtin_nontemporal_store(cv, reinterpret_cast<uint32_t*>(c.cv + i));
+      if ((threadIdx.x & 31) == 0) {
+        c.eu[i / Q8_BLOCK] = (uint8_t)eu;
+        c.ev[i / Q8_BLOCK] = (uint8_t)ev;
+      }
+    }
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float den = sqrtf(v[e] * s.inv_c2) + a.eps;
-    const float n = den == 0.f ? 0.f : u[e] * s.inv_c1 / den;        // den = 0: eps = 0 and no gradient so far
-    q.x[e] = fmaf(-a.lr, fmaf(s.wd, q.x[e], n), q.x[e]);
-  }
-  if (cnt == 4) store_quad<WBF, true>(w, i, q.x);
+  for (int e = 0; e < 4; ++e) q.x[e] = fmaf(-a.lr, fmaf(s.wd, q.x[e], update_of(u[e], v[e], s.inv_c1, s.inv_c2, a.eps)), q.x[e]);
+  if (cnt == 4) store_quad<WBF, true>(c.w, i, q.x);
   else
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (e < cnt) store_element<WBF>(w, i + e, q.x[e]);
+      if (e < cnt) store_element<WBF>(c.w, i + e, q.x[e]);
 }
 
 // The workgroup that is the last of its launch to come here.  Counters for a sixteenth of the workgroups each, so that few wait for one address; the last of each
@@ -282,10 +312,30 @@ __device__ __forceinline__ bool last_workgroup(int32_t* counters) {
 }
 
 constexpr int REPS = (int)(ADAMW_CHUNK / 1024), AHEAD = 2;      // quads of a thread, and how many of them are requested together
+template <bool WBF, bool Q8, int KIND>
+__device__ __forceinline__ void step_chunk(const AdamwArgs& a, const Chunk& c, const StepScalars& s) {
+  if (c.n == ADAMW_CHUNK) {
+#pragma unroll
+    for (int rep = 0; rep < REPS; rep += AHEAD) {
+      Quad<Q8> q[AHEAD];
+#pragma unroll
+      for (int r = 0; r < AHEAD; ++r) load_step<WBF, Q8, true, KIND>(q[r], c, (rep + r) * 1024 + threadIdx.x * 4);
+#pragma unroll
+      for (int r = 0; r < AHEAD; ++r) store_step<WBF, Q8, true>(q[r], a, c, s, (rep + r) * 1024 + threadIdx.x * 4);
+    }
+  } else {
+    for (int rep = 0; rep < REPS && rep * 1024 < c.n; ++rep) {
+      Quad<Q8> q;
+      load_step<WBF, Q8, false, KIND>(q, c, rep * 1024 + threadIdx.x * 4);
+      store_step<WBF, Q8, false>(q, a, c, s, rep * 1024 + threadIdx.x * 4);
+    }
+  }
+}
+
 template <bool WBF, bool Q8>
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
-  const int32_t c = a.first[0] + (int32_t)blockIdx.x;
-  const int k = find_tensor(a.first, a.count, c);
+  const int32_t chunk = a.first[0] + (int32_t)blockIdx.x;
+  const int k = find_tensor(a.first, a.count, chunk);
   const AdamwTensor t = a.tensors[k];
   const float coef = a.coef ? *a.coef : 1.f;
   if (!(fabsf(coef) < INFINITY)) {                     // the norm was not finite: this step is left out
@@ -293,37 +343,36 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
     return;
   }
   StepScalars s;
-  s.scale_d = a.scale * (double)coef;
-  s.scale = (float)s.scale_d;
+  const double scale = a.scale * (double)coef;
+  s.scale = (float)scale;
+  s.omb1_scale = a.omb1d * scale;
+  s.omb2_scale2 = a.omb2d * (scale * scale);
   s.inv_c1 = a.step->next_inv_c1; s.inv_c2 = a.step->next_inv_c2;
   s.wd = t.decay ? a.wd : 0.f;
   const int64_t steps = a.step->t;
-  s.turn = (uint32_t)(steps + 1) * STEP_TURN;
-  const int64_t base = (int64_t)(c - a.first[k]) * ADAMW_CHUNK;
-  void* const w = a.w[k];
-  const void* const g = a.g[k];
+  s.turn = (uint32_t)(steps + 1) * Q8_STEP;
+  const int64_t base = (int64_t)(chunk - a.first[k]) * ADAMW_CHUNK, at = t.off + base;
   const uint8_t kind = a.kind[k];
-  RowsOf rows{};
-  int64_t row0 = 0, col0 = 0;
+  const int dense = kind & G_ROWS ? 0 : kind & G_BF16 ? 2 : 4;         // bytes of an element of a dense gradient
+  Chunk c;
+  c.w = reinterpret_cast<char*>(a.w[k]) + base * (WBF ? 2 : 4);
+  c.g = reinterpret_cast<const char*>(a.g[k]) + base * dense;
+  c.rows = &a.rows[kind >> 2];
+  c.u = a.st.u + at; c.v = a.st.v + at;
+  c.cu = a.st.cu + at; c.cv = a.st.cv + at;
+  c.eu = a.st.eu + at / Q8_BLOCK; c.ev = a.st.ev + at / Q8_BLOCK;
+  c.cols = t.cols; c.row0 = c.col0 = 0;
+  c.n = (int32_t)std::min(t.n - base, ADAMW_CHUNK);
+  c.element = (uint32_t)base;
   if (kind & G_ROWS) {
-    rows = a.rows[kind >> 2];
-    row0 = base / t.cols; col0 = base - row0 * t.cols;
-  }
-  if (base + ADAMW_CHUNK <= t.n) {
-#pragma unroll
-    for (int rep = 0; rep < REPS; rep += AHEAD) {
-      Quad<Q8> q[AHEAD];
-#pragma unroll
-      for (int r = 0; r < AHEAD; ++r) load_step<WBF, Q8, true>(q[r], w, g, kind, rows, a.st, t, row0, col0, base, (rep + r) * 1024 + (int64_t)threadIdx.x * 4);
-#pragma unroll
-      for (int r = 0; r < AHEAD; ++r) store_step<WBF, Q8, true>(q[r], w, a, t, s, base, (rep + r) * 1024 + (int64_t)threadIdx.x * 4);
-    }
+    c.row0 = base / t.cols;
+    c.col0 = base - c.row0 * t.cols;
+    if (kind & G_BF16) step_chunk<WBF, Q8, ROWS_BF16>(a, c, s);
+    else step_chunk<WBF, Q8, ROWS_F32>(a, c, s);
+  } else if (kind & G_BF16) {
+    step_chunk<WBF, Q8, DENSE_BF16>(a, c, s);
   } else {
-    for (int rep = 0; rep < REPS && base + rep * 1024 < t.n; ++rep) {
-      Quad<Q8> q;
-      load_step<WBF, Q8, false>(q, w, g, kind, rows, a.st, t, row0, col0, base, rep * 1024 + (int64_t)threadIdx.x * 4);
-      store_step<WBF, Q8, false>(q, w, a, t, s, base, rep * 1024 + (int64_t)threadIdx.x * 4);
-    }
+    step_chunk<WBF, Q8, DENSE_F32>(a, c, s);
   }
   if (!a.advance) return;
   // t <- t + 1, once every workgroup has read what belongs to t
@@ -335,45 +384,65 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
 // between the tensors is written as zero.
 template <bool Q8, bool TO_STATE>
 __global__ __launch_bounds__(256) void k_moments(AdamwState st, const AdamwTensor* tensors, const int32_t* first, int32_t count, float* plain, int64_t total) {
-  const int32_t c = (int32_t)blockIdx.x;
-  int k = 0;                                          // (any number of tensors: search by halves)
-  for (int lo = 0, hi = count; hi - lo > 1;) {
-    const int mid = (lo + hi) / 2;
-    if (first[mid] <= c) lo = mid; else hi = mid;
-    k = lo;
-  }
+  const int32_t chunk = first[0] + (int32_t)blockIdx.x;
+  const int k = find_tensor(first, count, chunk);
   const AdamwTensor t = tensors[k];
-  const int64_t base = (int64_t)(c - first[k]) * ADAMW_CHUNK, padded = (t.n + Q8_BLOCK - 1) / Q8_BLOCK * Q8_BLOCK;
-  for (int rep = 0; rep < (int)(ADAMW_CHUNK / 1024); ++rep) {
-    const int64_t i = base + rep * 1024 + (int64_t)threadIdx.x * 4, at = t.off + i;
-    if (base + rep * 1024 >= padded) break;
+  const int64_t base = (int64_t)(chunk - first[k]) * ADAMW_CHUNK, at = t.off + base;
+  const int32_t n = (int32_t)std::min(t.n - base, ADAMW_CHUNK), padded = (n + Q8_BLOCK - 1) / Q8_BLOCK * Q8_BLOCK;
+  float* const pu = plain + at;
+  float* const pv = plain + total + at;
+  for (int rep = 0; rep < REPS && rep * 1024 < padded; ++rep) {
+    const int i = rep * 1024 + (int)threadIdx.x * 4, cnt = std::min(std::max(n - i, 0), 4);
     const bool any = i < padded;
     float u[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (any && (TO_STATE || !Q8)) {
-      for (int e = 0; e < 4; ++e)
-        if (i + e < t.n) {
-          u[e] = TO_STATE ? plain[at + e] : st.u[at + e];
-          v[e] = TO_STATE ? plain[total + at + e] : st.v[at + e];
+    if constexpr (TO_STATE) {
+      if (cnt == 4) {
+        load_quad<false, true>(pu, i, u);
+        load_quad<false, true>(pv, i, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < cnt) { u[e] = pu[i + e]; v[e] = pv[i + e]; }
+      }
+      if constexpr (Q8) {
+        double du[4], dv[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { du[e] = (double)u[e]; v[e] = fabsf(v[e]); dv[e] = (double)v[e]; }
+        int eu, ev;
+        auto half = [](int) { return 1u << 16; };
+        const uint32_t cu = q8_encode<true>(du, u, half, eu), cv = q8_encode<false>(dv, v, half, ev);
+        if (any) {
+          *reinterpret_cast<uint32_t*>(st.cu + at + i) = cu;
+          *reinterpret_cast<uint32_t*>(st.cv + at + i) = cv;
+          if ((threadIdx.x & 31) == 0) {
+            st.eu[(at + i) / Q8_BLOCK] = (uint8_t)eu;
+            st.ev[(at + i) / Q8_BLOCK] = (uint8_t)ev;
+          }
         }
-    }
-    if constexpr (Q8 && TO_STATE) {
-      const double du[4] = {u[0], u[1], u[2], u[3]}, dv[4] = {v[0], v[1], v[2], v[3]};
-      const uint32_t none[4] = {};
-      q8_store<true>(st, at, any, du, dv, none);
+      } else if (any) {
+        *reinterpret_cast<f32x4a*>(st.u + at + i) = f32x4a{u[0], u[1], u[2], u[3]};
+        *reinterpret_cast<f32x4a*>(st.v + at + i) = f32x4a{v[0], v[1], v[2], v[3]};
+      }
     } else if (any) {
       if constexpr (Q8) {
-        const uint32_t cu = *reinterpret_cast<const uint32_t*>(st.cu + at), cv = *reinterpret_cast<const uint32_t*>(st.cv + at);
-        const int eu = st.eu[at / Q8_BLOCK], ev = st.ev[at / Q8_BLOCK];
+        const int eu = st.eu[(at + i) / Q8_BLOCK], ev = st.ev[(at + i) / Q8_BLOCK];
+        double du[4], dv[4];
+        q8_decode<true>(*reinterpret_cast<const uint32_t*>(st.cu + at + i), eu, du);
+        q8_decode<false>(*reinterpret_cast<const uint32_t*>(st.cv + at + i), ev, dv);
+#pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (i + e < t.n) {
-            const double x = q8_value((cu >> (8 * e)) & 0x7f, 127, eu);
-            u[e] = (float)((cu >> (8 * e)) & 0x80 ? -x : x);
-            v[e] = (float)q8_value((cv >> (8 * e)) & 0xff, 255, ev);
+          if (e < cnt) {
+            u[e] = eu == Q8_NAN ? NAN : (float)du[e];
+            v[e] = ev == Q8_NAN ? NAN : (float)dv[e];
           }
+      } else {
+        const f32x4a x = *reinterpret_cast<const f32x4a*>(st.u + at + i), y = *reinterpret_cast<const f32x4a*>(st.v + at + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < cnt) { u[e] = x[e]; v[e] = y[e]; }
       }
-      float* du = TO_STATE ? st.u + at : plain + at;
-      float* dv = TO_STATE ? st.v + at : plain + total + at;
-      for (int e = 0; e < 4; ++e) { du[e] = u[e]; dv[e] = v[e]; }
+      store_quad<false, true>(pu, i, u);
+      store_quad<false, true>(pv, i, v);
     }
   }
 }
@@ -552,6 +621,7 @@ int plan_adamw(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams
   if (!tensors || !hp || n <= 0) return LORDO_EINVAL;
   if (!unit(hp->beta1) || !unit(hp->beta2) || !(hp->eps >= 0) || !std::isfinite(hp->eps) || !(hp->weight_decay >= 0) || !std::isfinite(hp->weight_decay))
     return LORDO_EINVAL;
+  if (hp->eps > 0 && hp->eps < 0x1p-126) return LORDO_EINVAL;           // (see update_of)
   if (hp->bias_correction != 0 && hp->bias_correction != 1) return LORDO_EINVAL;
   if (hp->param_dtype != LORDO_F32 && hp->param_dtype != LORDO_BF16) return LORDO_EINVAL;
   if ((hp->state_dtype != LORDO_F32 && hp->state_dtype != LORDO_Q8) || hp->reserved != 0) return LORDO_EINVAL;
@@ -611,19 +681,24 @@ uint8_t grad_kind(const lordo_grad& g, int rows) { return (uint8_t)((g.dtype == 
   } while (0)
 
 int moments(lordo_adamw* c, float* plain, bool to_state, hipStream_t s) {
-  const AdamwTensor* tensors = reinterpret_cast<const AdamwTensor*>(c->arena + c->table);
-  const int32_t* first = reinterpret_cast<const int32_t*>(c->arena + c->prefix);
-  const int32_t n = (int32_t)c->shapes.size();
-  const dim3 grid((unsigned)c->first.back()), block(256);
+  const int n = (int)c->shapes.size();
   const AdamwState st = c->state();
-  if (c->hp.state_dtype == LORDO_Q8) {
-    if (to_state) hipLaunchKernelGGL((k_moments<true, true>), grid, block, 0, s, st, tensors, first, n, plain, c->total);
-    else hipLaunchKernelGGL((k_moments<true, false>), grid, block, 0, s, st, tensors, first, n, plain, c->total);
-  } else {
-    if (to_state) hipLaunchKernelGGL((k_moments<false, true>), grid, block, 0, s, st, tensors, first, n, plain, c->total);
-    else hipLaunchKernelGGL((k_moments<false, false>), grid, block, 0, s, st, tensors, first, n, plain, c->total);
+  for (int at = 0; at < n; at += 256) {
+    const AdamwTensor* tensors = reinterpret_cast<const AdamwTensor*>(c->arena + c->table) + at;
+    const int32_t* first = reinterpret_cast<const int32_t*>(c->arena + c->prefix) + at;
+    const int count = std::min(256, n - at);
+    const dim3 grid((unsigned)(c->first[at + count] - c->first[at])), block(256);
+    if (c->hp.state_dtype == LORDO_Q8) {
+      if (to_state) hipLaunchKernelGGL((k_moments<true, true>), grid, block, 0, s, st, tensors, first, count, plain, c->total);
+      else hipLaunchKernelGGL((k_moments<true, false>), grid, block, 0, s, st, tensors, first, count, plain, c->total);
+    } else {
+      if (to_state) hipLaunchKernelGGL((k_moments<false, true>), grid, block, 0, s, st, tensors, first, count, plain, c->total);
+      else hipLaunchKernelGGL((k_moments<false, false>), grid, block, 0, s, st, tensors, first, count, plain, c->total);
+    }
+    const int rc = launched("k_moments");
+    if (rc != LORDO_OK) return rc;
   }
-  return launched("k_moments");
+  return LORDO_OK;
 }
 
 }  // namespace

@@ -54,7 +54,10 @@ def in_8_bits(x, w, signed):
         if not most <= 2.0 ** 127:
             out[b:b + BLOCK] = np.nan
             continue
-        scale = 2.0 ** max(math.ceil(math.log2(most)), -126) if most > 0 else 1.0
+        if most == 0:
+            out[b:b + BLOCK] = 0
+            continue
+        scale = 2.0 ** max(math.ceil(math.log2(most)), -126)
         y = np.minimum(np.abs(part) / scale, 1.0)
         m, e = np.frexp(y)
         eighths = (2 * m - 1) * 8
