@@ -110,23 +110,26 @@ template <bool SIGNED, class W>
 __device__ __forceinline__ uint32_t q8_encode(const double (&x)[4], const float (&x32)[4], W w, int& exponent) {
   uint32_t most = 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(x32[e]) & 0x7fffffffu);
+  for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(x32[e]) & (SIGNED ? 0x7fffffffu : 0xffffffffu));
   exponent = q8_exponent(max32(most));
   const int top = 8 * (exponent + 1023 - 127) - (SIGNED ? 127 : 255);
   const uint32_t some = exponent == 0 ? 0 : SIGNED ? 0x7f : 0xff;               // nothing that fp32 holds: zeros
   int code[4];
-  uint32_t low = 0;
+  uint32_t least = 0xffffffffu;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const uint32_t m = (uint32_t)__double2hiint(x[e]) & 0x7fffffffu;
-    code[e] = (int)((m + w(e)) >> 17) - top;
-    if constexpr (!SIGNED) code[e] = max(code[e], 1);
-    code[e] = m ? code[e] : 0;
-    // 1.25 2^-16 of 2^E in the upper half of a double: below it, but not zero
-    if constexpr (SIGNED) low |= (uint32_t)(m - 1 < (((uint32_t)(exponent + 1023 - 127 - 16) << 20) | 2u << 17) - 1);
+    code[e] = (int)((m + w(e)) >> 17) - top;           // far below 0 for a zero
+    if constexpr (SIGNED) {
+      code[e] = max(code[e], 0);
+      least = min(least, m - 1);                       // (a zero is above all)
+    } else {
+      code[e] = min(max(code[e], 1), (int)m);
+    }
   }
   if constexpr (SIGNED) {
-    if (__any(low)) {
+    // 1.25 2^-16 of 2^E in the upper half of a double
+    if (__any(least < (((uint32_t)(exponent + 1023 - 127 - 16) << 20) | 2u << 17) - 1)) {
       constexpr double LEAST = 1.25 / 65536.0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -236,13 +239,28 @@ struct StepScalars {
   uint32_t turn;
 };
 
-// (u / c1) / (sqrt(v / c2) + eps) by the approximate root and reciprocal (one unit in the last place each): the root's argument is brought out of the
-// subnormal range, which the instruction does not take, and so is no sum with eps in it (the host refuses an eps there).
-__device__ __forceinline__ float update_of(float u, float v, float inv_c1, float inv_c2, float eps) {
-  const float x = v * inv_c2;
-  const bool small = x < 0x1p-96f;
-  const float den = fmaf(__builtin_amdgcn_sqrtf(small ? x * 0x1p64f : x), small ? 0x1p-32f : 1.f, eps);
-  return den == 0.f ? 0.f : u * inv_c1 * __builtin_amdgcn_rcpf(den);       // den = 0: eps = 0 and no gradient so far
+// (u / c1) / (sqrt(v / c2) + eps) by the approximate root and reciprocal (one unit in the last place each).  Neither takes subnormal numbers: in a wave that
+// has a root of one, its argument is scaled; a sum with eps is none, as the host refuses an eps there; and with eps = 0 a sum of 0 means no gradient so far.
+__device__ __forceinline__ void updates_of(const float (&u)[4], const float (&v)[4], float inv_c1, float inv_c2, float eps, float (&n)[4]) {
+  float x[4], den[4];
+  uint32_t least = 0xffffffffu;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = v[e] * inv_c2;
+    least = min(least, __float_as_uint(x[e]) - 1);     // (a zero is above all)
+    den[e] = __builtin_amdgcn_sqrtf(x[e]) + eps;
+  }
+  if (__any(least < __float_as_uint(0x1p-96f) - 1)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (x[e] < 0x1p-96f) den[e] = fmaf(__builtin_amdgcn_sqrtf(x[e] * 0x1p64f), 0x1p-32f, eps);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) n[e] = u[e] * inv_c1 * __builtin_amdgcn_rcpf(den[e]);
+  if (eps == 0.f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) n[e] = den[e] == 0.f ? 0.f : n[e];
+  }
 }
 
 template <bool WBF, bool Q8, bool WHOLE>
@@ -290,8 +308,10 @@ __device__ __forceinline__ void store_step(Quad<Q8>& q, const AdamwArgs& a, cons
       }
     }
   }
+  float n[4];
+  updates_of(u, v, s.inv_c1, s.inv_c2, a.eps, n);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) q.x[e] = fmaf(-a.lr, fmaf(s.wd, q.x[e], update_of(u[e], v[e], s.inv_c1, s.inv_c2, a.eps)), q.x[e]);
+  for (int e = 0; e < 4; ++e) q.x[e] = fmaf(-a.lr, fmaf(s.wd, q.x[e], n[e]), q.x[e]);
   if (cnt == 4) store_quad<WBF, true>(c.w, i, q.x);
   else
 #pragma unroll
@@ -621,7 +641,7 @@ int plan_adamw(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams
   if (!tensors || !hp || n <= 0) return LORDO_EINVAL;
   if (!unit(hp->beta1) || !unit(hp->beta2) || !(hp->eps >= 0) || !std::isfinite(hp->eps) || !(hp->weight_decay >= 0) || !std::isfinite(hp->weight_decay))
     return LORDO_EINVAL;
-  if (hp->eps > 0 && hp->eps < 0x1p-126) return LORDO_EINVAL;           // (see update_of)
+  if (hp->eps > 0 && hp->eps < 0x1p-126) return LORDO_EINVAL;           // (see updates_of)
   if (hp->bias_correction != 0 && hp->bias_correction != 1) return LORDO_EINVAL;
   if (hp->param_dtype != LORDO_F32 && hp->param_dtype != LORDO_BF16) return LORDO_EINVAL;
   if ((hp->state_dtype != LORDO_F32 && hp->state_dtype != LORDO_Q8) || hp->reserved != 0) return LORDO_EINVAL;
