@@ -331,9 +331,12 @@ __device__ __forceinline__ bool last_workgroup(int32_t* counters) {
   return true;
 }
 
-constexpr int REPS = (int)(ADAMW_CHUNK / 1024), AHEAD = 2;      // quads of a thread, and how many of them are requested together
+constexpr int REPS = (int)(ADAMW_CHUNK / 1024);                 // quads of a thread
 template <bool WBF, bool Q8, int KIND>
 __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const Chunk& c, const StepScalars& s) {
+  // Quads requested together.  fp32 moments: bound by memory, all four of a chunk (embedding and head of a 1B model in us: 1 518, 2 507, 4 497; with
+  // chunks of 2048, 2 498).  8 bits: bound by instructions, and with the registers of more of them fewer waves fit (1 1000, 2 1019, 4 1009; all with the export).
+  constexpr int AHEAD = Q8 ? 1 : REPS;
   if (c.n == ADAMW_CHUNK) {
 #pragma unroll
     for (int rep = 0; rep < REPS; rep += AHEAD) {

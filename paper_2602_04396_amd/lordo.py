@@ -394,31 +394,36 @@ class Lordo:
 
 # ---- what a model has beside its projected matrices: AdamW, gradient norm, token embedding ------------------------------
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
-def _same_device(*tensors):
-    """The one GPU all of them are on, which has to be current: the calls without a context enqueue there."""
-    dev = tensors[0].device
-    if dev.type != "cuda" or any(t.device != dev for t in tensors):
-        raise ValueError("expected CUDA tensors on one device")
-    if dev.index != _torch().cuda.current_device():
-        raise ValueError(f"tensors are on {dev}, which is not the current device")
-    return dev
+def _same_device(torch, *tensors):
+    """Refuses tensors that are not on the current GPU: the calls without a context enqueue there."""
+    at = torch.cuda.current_device() if tensors[0].is_cuda else -1
+    for t in tensors:
+        if t.get_device() != at or at < 0:
+            raise ValueError("expected CUDA tensors on the current device, got " + ", ".join(str(t.device) for t in tensors))
 
 
 def _stream_of(torch):
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _float_code(t, torch):
-    if t.dtype == torch.float32:
+    dtype = t.dtype
+    if dtype is torch.float32:
         return F32
-    if t.dtype == torch.bfloat16:
+    if dtype is torch.bfloat16:
         return BF16
-    raise ValueError(f"expected a float32 or bfloat16 tensor, got {t.dtype}")
+    raise ValueError(f"expected a float32 or bfloat16 tensor, got {dtype}")
 
 
 def _rows_cols(t):
@@ -462,8 +467,8 @@ class GradList:
             if not data.is_contiguous():
                 raise ValueError("expected contiguous gradients")
             flat.append(data)
-        self.device = flat[0].device
-        if self.device.type != "cuda" or any(t.device != self.device for t in flat):
+        self.device, self.at = flat[0].device, flat[0].get_device()
+        if self.at < 0 or any(t.get_device() != self.at for t in flat):
             raise ValueError("expected CUDA tensors on one device")
 
     def __len__(self):
@@ -478,16 +483,18 @@ def grad_norm(grads, max_norm=float("inf"), out=None):
     """Tensor of two floats on the device: the norm over all gradients, and min(1, max_norm / norm) (Alg. 1 clip; NaN if the norm is not finite).
     AdamW.local_step takes it as `clip`; Lordo.local_step takes its second value, read back, as grad_scale."""
     torch = _torch()
-    grads = grad_list(grads)
-    if grads.device.index != torch.cuda.current_device():
+    if not isinstance(grads, GradList):
+        grads = GradList(grads)
+    if grads.at != torch.cuda.current_device():
         raise ValueError(f"tensors are on {grads.device}, which is not the current device")
+    # the result and, from 256 bytes on, the workspace in one allocation
+    room = torch.empty(64 + NORM_WORKSPACE_BYTES // 4, dtype=torch.float32, device=grads.device)
+    at = room.data_ptr()
     if out is None:
-        out = torch.empty(2, dtype=torch.float32, device=grads.device)
+        out = room[:2]
     elif out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous() or out.device != grads.device:
         raise ValueError("expected a contiguous float32 tensor of two elements on the gradients' device")
-    ws = torch.empty(NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=grads.device)
-    _check(load().lordo_grad_norm(grads.arr, len(grads), float(max_norm), C.c_void_p(out.data_ptr()), C.c_void_p(ws.data_ptr()), NORM_WORKSPACE_BYTES,
-                                  _stream_of(torch)))
+    _check(load().lordo_grad_norm(grads.arr, len(grads.grads), max_norm, out.data_ptr(), at + 256, NORM_WORKSPACE_BYTES, _stream_of(torch)))
     return out
 
 
@@ -500,7 +507,8 @@ class AdamW:
         self.ctx = C.c_void_p()
         self.shapes = [tuple(sh) for sh in shapes]
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-        if self.device.index != torch.cuda.current_device():
+        self.at = self.device.index
+        if self.at != torch.cuda.current_device():
             raise ValueError(f"{self.device} is not the current device")
         arr = (Tensor * len(self.shapes))()
         for a, sh in zip(arr, self.shapes):
@@ -528,13 +536,18 @@ class AdamW:
 
     def local_step(self, W, G, lr, grad_scale=1.0, clip=None):
         """One step; the gradient is grad_scale * clip[1] * G (clip: what grad_norm returned, or None)."""
-        W, G = self.ptrs(W), grad_list(G)
-        if len(G) != len(self.shapes) or G.device != self.device:
+        if not isinstance(W, PtrList):
+            W = self.ptrs(W)
+        if not isinstance(G, GradList):
+            G = GradList(G)
+        if len(G.grads) != len(self.shapes) or G.at != self.at:
             raise ValueError(f"expected one gradient per shape on {self.device}")
-        if clip is not None and (clip.dtype != self.torch.float32 or clip.numel() != 2 or not clip.is_contiguous() or clip.device != self.device):
-            raise ValueError("clip: expected the two floats of grad_norm")
-        _check(self.lib.lordo_adamw_step(self.ctx, W.arr, G.arr, float(lr), float(grad_scale),
-                                         None if clip is None else C.c_void_p(clip.data_ptr()), self._stream()))
+        at = None
+        if clip is not None:
+            if clip.dtype is not self.torch.float32 or clip.numel() != 2 or not clip.is_contiguous() or clip.get_device() != self.at:
+                raise ValueError("clip: expected the two floats of grad_norm")
+            at = clip.data_ptr()
+        _check(self.lib.lordo_adamw_step(self.ctx, W.arr, G.arr, lr, grad_scale, at, _stream_of(self.torch)))
 
     def _moments(self):
         ptr, count = C.c_void_p(), C.c_size_t()
@@ -593,9 +606,11 @@ class AdamW:
 
 
 def _ids(ids, torch):
-    if ids.dtype not in (torch.int64, torch.int32) or not ids.is_contiguous():
+    """Address, type code and number of token ids."""
+    dtype = ids.dtype
+    if (dtype is not torch.int64 and dtype is not torch.int32) or not ids.is_contiguous():
         raise ValueError("expected contiguous int32 or int64 token ids")
-    return C.c_void_p(ids.data_ptr()), I64 if ids.dtype == torch.int64 else I32, ids.numel()
+    return ids.data_ptr(), I64 if dtype is torch.int64 else I32, ids.numel()
 
 
 def embed_lookup(table, ids, scale=1.0, out=None, dtype=None):
@@ -604,21 +619,22 @@ def embed_lookup(table, ids, scale=1.0, out=None, dtype=None):
     if table.dim() != 2 or not table.is_contiguous():
         raise ValueError("expected a contiguous (vocab, cols) table")
     p, code, n = _ids(ids, torch)
-    want = tuple(ids.shape) + (table.shape[1],)
+    vocab, cols = table.shape
     if out is None:
-        out = torch.empty(want, dtype=dtype or table.dtype, device=table.device)
-    elif tuple(out.shape) != want or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
-        raise ValueError(f"expected a contiguous output of shape {want}")
-    _same_device(table, ids, out)
-    _check(load().lordo_embed_lookup(C.c_void_p(table.data_ptr()), _float_code(table, torch), table.shape[0], table.shape[1], p, code, n, float(scale),
-                                     C.c_void_p(out.data_ptr()), _float_code(out, torch), _stream_of(torch)))
+        out = torch.empty((*ids.shape, cols), dtype=dtype or table.dtype, device=table.device)
+    elif tuple(out.shape) != (*ids.shape, cols) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"expected a contiguous output of shape {(*ids.shape, cols)}")
+    _same_device(torch, table, ids, out)
+    _check(load().lordo_embed_lookup(table.data_ptr(), _float_code(table, torch), vocab, cols, p, code, n, scale, out.data_ptr(),
+                                     _float_code(out, torch), _stream_of(torch)))
     return out
 
 
-def _gradient_args(ids, dy, vocab, torch):
+def _workspace(ids, dy, vocab, torch):
+    """Columns of dy, and bytes and tensor of the workspace of its gradient."""
     cols = dy.shape[-1]
-    if tuple(dy.shape[:-1]) != tuple(ids.shape) or not dy.is_contiguous():
-        raise ValueError(f"expected a contiguous gradient of shape {tuple(ids.shape) + (cols,)}")
+    if dy.shape[:-1] != ids.shape or not dy.is_contiguous():
+        raise ValueError(f"expected a contiguous gradient of shape {(*ids.shape, cols)}")
     size = C.c_size_t(0)
     _check(load().lordo_embed_workspace_bytes(ids.numel(), vocab, cols, C.byref(size)))
     return cols, size.value, torch.empty(size.value, dtype=torch.uint8, device=dy.device)
@@ -629,24 +645,22 @@ def embed_gradient(ids, dy, out, scale=1.0, pad_id=-1, accumulate=False):
     torch = _torch()
     if out.dim() != 2 or not out.is_contiguous() or dy.shape[-1] != out.shape[1]:
         raise ValueError("expected a contiguous (vocab, cols) output")
-    _same_device(ids, dy, out)
+    _same_device(torch, ids, dy, out)
     p, code, n = _ids(ids, torch)
-    cols, size, ws = _gradient_args(ids, dy, out.shape[0], torch)
-    _check(load().lordo_embed_gradient(p, code, n, C.c_void_p(dy.data_ptr()), _float_code(dy, torch), out.shape[0], cols, float(scale), int(pad_id),
-                                       int(accumulate), C.c_void_p(out.data_ptr()), _float_code(out, torch), C.c_void_p(ws.data_ptr()), size,
-                                       _stream_of(torch)))
+    cols, size, ws = _workspace(ids, dy, out.shape[0], torch)
+    _check(load().lordo_embed_gradient(p, code, n, dy.data_ptr(), _float_code(dy, torch), out.shape[0], cols, scale, pad_id, int(accumulate),
+                                       out.data_ptr(), _float_code(out, torch), ws.data_ptr(), size, _stream_of(torch)))
     return out
 
 
 def embed_gradient_rows(ids, dy, vocab, scale=1.0, pad_id=-1, dtype=None) -> RowGrad:
     """Gradient of embed_lookup by rows, for AdamW.local_step and grad_norm: one row per different token, of `dtype` (float32 if None)."""
     torch = _torch()
-    _same_device(ids, dy)
+    _same_device(torch, ids, dy)
     p, code, n = _ids(ids, torch)
-    cols, size, ws = _gradient_args(ids, dy, vocab, torch)
+    cols, size, ws = _workspace(ids, dy, vocab, torch)
     rows = torch.empty((n, cols), dtype=dtype or torch.float32, device=dy.device)
     index = torch.empty(vocab + n, dtype=torch.int32, device=dy.device)
-    _check(load().lordo_embed_gradient_rows(p, code, n, C.c_void_p(dy.data_ptr()), _float_code(dy, torch), vocab, cols, float(scale), int(pad_id),
-                                            C.c_void_p(rows.data_ptr()), _float_code(rows, torch), C.c_void_p(index.data_ptr()),
-                                            C.c_void_p(ws.data_ptr()), size, _stream_of(torch)))
+    _check(load().lordo_embed_gradient_rows(p, code, n, dy.data_ptr(), _float_code(dy, torch), vocab, cols, scale, pad_id, rows.data_ptr(),
+                                            _float_code(rows, torch), index.data_ptr(), ws.data_ptr(), size, _stream_of(torch)))
     return RowGrad(rows, index, vocab)
