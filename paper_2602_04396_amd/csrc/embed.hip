@@ -34,23 +34,31 @@ __device__ __forceinline__ int32_t token_key(const Ids& ids, int64_t t) {
   return id < 0 || id >= ids.vocab || id == ids.pad_id ? ids.vocab : (int32_t)id;
 }
 
-template <bool IN_BF, bool OUT_BF>
+// A thread copies eight columns of ROWS rows, all requested before the first is written.  NARROW: rows shorter than that, a thread an element.
+template <bool IN_BF, bool OUT_BF, int ROWS, bool NARROW>
 __global__ __launch_bounds__(256) void k_lookup(const void* table, Ids ids, int64_t tokens, int64_t cols, int lanes_log2, float scale, void* out) {
-  const int lanes = 1 << lanes_log2;                                   // threads of a row
-  const int64_t t = (int64_t)blockIdx.x * (256 >> lanes_log2) + (threadIdx.x >> lanes_log2);
-  if (t >= tokens) return;
-  const int32_t id = token_key(ids, t);
-  const int64_t from = (int64_t)id * cols, to = t * cols;
-  for (int64_t c = (int64_t)(threadIdx.x & (lanes - 1)) * 4; c < cols; c += (int64_t)lanes * 4) {
-    const int cnt = cols - c >= 4 ? 4 : (int)(cols - c);
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (cnt == 4) {
-      if (id < ids.vocab) load_quad<IN_BF, false>(table, from + c, x);
-      for (int e = 0; e < 4; ++e) x[e] *= scale;
-      store_quad<OUT_BF, false>(out, to + c, x);
-    } else {
-      for (int e = 0; e < cnt; ++e) store_element<OUT_BF>(out, to + c + e, id < ids.vocab ? load_element<IN_BF>(table, from + c + e) * scale : 0.f);
-    }
+  constexpr int VEC = NARROW ? 1 : 8;
+  const int lanes = 1 << lanes_log2, per = 256 >> lanes_log2;          // threads of a row, rows of a workgroup at a time
+  const int64_t c0 = ((int64_t)blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * VEC;
+  if (c0 >= cols) return;
+  const int64_t c = std::min(c0, cols - VEC);                          // the last piece of a row ends where the row does
+  const int64_t first = (int64_t)blockIdx.x * per * ROWS + (threadIdx.x >> lanes_log2);
+  int32_t id[ROWS];
+  Piece<IN_BF, VEC> x[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) id[r] = first + r * per < tokens ? token_key(ids, first + r * per) : ids.vocab;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    x[r].clear();
+    if (id[r] < ids.vocab) x[r].load(table, (int64_t)id[r] * cols + c);
+  }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (first + r * per >= tokens) break;
+    float y[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) y[e] = x[r].value(e) * scale;
+    put_piece<OUT_BF, VEC>(out, (first + r * per) * cols + c, y, (int)(c0 - c));
   }
 }
 
@@ -230,24 +238,6 @@ struct GradOut {
   int32_t add;
 };
 
-// Elements skip ... VEC - 1 of a piece (what comes before them is the neighbour's).
-template <bool BF, int VEC>
-__device__ __forceinline__ void put_piece(void* p, int64_t at, const float (&x)[VEC], int skip) {
-  if constexpr (VEC >= 4) {
-    if (skip == 0) {
-#pragma unroll
-      for (int h = 0; h < VEC; h += 4) {
-        const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
-        store_quad<BF, false>(p, at + h, y);
-      }
-      return;
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < VEC; ++e)
-    if (e >= skip) store_element<BF>(p, at + e, x[e]);
-}
-
 // A workgroup sums the runs of one id that begin in its tile of sorted tokens, a thread sixteen bytes of columns.  A run that ends in the next tile is summed here to its
 // end, so a tile works on at most two tiles of tokens and only longer runs leave partial rows: one of the tile they begin in (slot 1), one
 // of each tile they go on in (slot 0).  Every wave holds ids and positions of both tiles, a lane one; rows are requested eight at a time, with
@@ -392,6 +382,28 @@ bool good_ids(const void* ids, int32_t dtype, int64_t tokens) {
 bool good_table(int64_t vocab, int64_t cols) { return vocab > 0 && vocab <= LORDO_MAX_VOCAB && cols > 0 && cols <= LORDO_MAX_EMBED_COLS; }
 int64_t up256(int64_t x) { return (x + 255) & ~int64_t(255); }
 
+template <bool IN_BF, bool OUT_BF>
+void launch_lookup_as(const void* table, Ids ids, int64_t tokens, int64_t cols, float scale, void* out, hipStream_t s) {
+  const bool narrow = cols < 8;
+  const int64_t pieces = narrow ? cols : (cols + 7) / 8;
+  int lanes_log2 = 0;
+  while (lanes_log2 < 8 && (int64_t(1) << lanes_log2) < pieces) ++lanes_log2;
+  const int64_t per = 256 >> lanes_log2, columns = (pieces + (int64_t(1) << lanes_log2) - 1) >> lanes_log2;
+  // four rows a thread once that leaves eight workgroups a compute unit
+  const int rows = (tokens + per - 1) / per * columns >= 8192 ? 4 : 1;
+  const dim3 grid((unsigned)((tokens + per * rows - 1) / (per * rows)), (unsigned)columns), block(256);
+  if (narrow && rows == 4) hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, 4, true>), grid, block, 0, s, table, ids, tokens, cols, lanes_log2, scale, out);
+  else if (narrow) hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, 1, true>), grid, block, 0, s, table, ids, tokens, cols, lanes_log2, scale, out);
+  else if (rows == 4) hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, 4, false>), grid, block, 0, s, table, ids, tokens, cols, lanes_log2, scale, out);
+  else hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, 1, false>), grid, block, 0, s, table, ids, tokens, cols, lanes_log2, scale, out);
+}
+void launch_lookup(const void* table, bool in_bf, Ids ids, int64_t tokens, int64_t cols, float scale, void* out, bool out_bf, hipStream_t s) {
+  if (in_bf && out_bf) launch_lookup_as<true, true>(table, ids, tokens, cols, scale, out, s);
+  else if (in_bf) launch_lookup_as<true, false>(table, ids, tokens, cols, scale, out, s);
+  else if (out_bf) launch_lookup_as<false, true>(table, ids, tokens, cols, scale, out, s);
+  else launch_lookup_as<false, false>(table, ids, tokens, cols, scale, out, s);
+}
+
 // Threads of a row of k_tile_sum, and tokens of its tiles: as many as leave 4096 waves (four a SIMD), 8 to 32.
 struct GradShape { int64_t pieces; unsigned threads; int tile; bool narrow; };
 GradShape gradient_shape(int64_t tokens, int64_t cols, bool in_bf) {
@@ -510,17 +522,7 @@ int lordo_embed_lookup(const void* table, int32_t table_dtype, int64_t vocab, in
   if (tokens == 0) return LORDO_OK;
   if (!table || !out || !float_aligned(table, table_dtype) || !float_aligned(out, out_dtype)) return LORDO_EINVAL;
   const Ids id{ids, ids_dtype == LORDO_I64, (int32_t)vocab, -1};
-  int lanes_log2 = 0;
-  while (lanes_log2 < 8 && (int64_t(4) << lanes_log2) < cols) ++lanes_log2;
-  const int64_t per_block = 256 >> lanes_log2;
-  const dim3 grid((unsigned)((tokens + per_block - 1) / per_block)), block(256);
-  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const float f = (float)scale;
-  const bool in_bf = table_dtype == LORDO_BF16, out_bf = out_dtype == LORDO_BF16;
-  if (in_bf && out_bf) hipLaunchKernelGGL((k_lookup<true, true>), grid, block, 0, s, table, id, tokens, cols, lanes_log2, f, out);
-  else if (in_bf) hipLaunchKernelGGL((k_lookup<true, false>), grid, block, 0, s, table, id, tokens, cols, lanes_log2, f, out);
-  else if (out_bf) hipLaunchKernelGGL((k_lookup<false, true>), grid, block, 0, s, table, id, tokens, cols, lanes_log2, f, out);
-  else hipLaunchKernelGGL((k_lookup<false, false>), grid, block, 0, s, table, id, tokens, cols, lanes_log2, f, out);
+  launch_lookup(table, table_dtype == LORDO_BF16, id, tokens, cols, (float)scale, out, out_dtype == LORDO_BF16, reinterpret_cast<hipStream_t>(stream));
   return launched("k_lookup");
 }
 

@@ -75,6 +75,7 @@ struct Piece;
 template <>
 struct Piece<false, 4> {
   f32x4u v;
+  __device__ __forceinline__ void clear() { v = f32x4u{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const f32x4u*>(reinterpret_cast<const float*>(p) + at); }
   __device__ __forceinline__ float value(int e) const { return v[e]; }
 };
@@ -88,20 +89,41 @@ template <>
 struct Piece<true, 8> {
   u32x4u v;
   __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const u32x4u*>(reinterpret_cast<const uint16_t*>(p) + at); }
+  __device__ __forceinline__ void clear() { v = u32x4u{0, 0, 0, 0}; }
   __device__ __forceinline__ float value(int e) const { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
 };
 template <>
 struct Piece<false, 8> {
   Piece<false, 4> v[2];
   __device__ __forceinline__ void load(const void* p, int64_t at) { v[0].load(p, at); v[1].load(p, at + 4); }
+  __device__ __forceinline__ void clear() { v[0].clear(); v[1].clear(); }
   __device__ __forceinline__ float value(int e) const { return v[e / 4].value(e & 3); }
 };
 template <bool BF>
 struct Piece<BF, 1> {
   float v;
   __device__ __forceinline__ void load(const void* p, int64_t at) { v = load_element<BF>(p, at); }
+  __device__ __forceinline__ void clear() { v = 0.f; }
   __device__ __forceinline__ float value(int) const { return v; }
 };
+
+// Elements skip ... VEC - 1 of a piece (what comes before them is the neighbour's).
+template <bool BF, int VEC>
+__device__ __forceinline__ void put_piece(void* p, int64_t at, const float (&x)[VEC], int skip) {
+  if constexpr (VEC >= 4) {
+    if (skip == 0) {
+#pragma unroll
+      for (int h = 0; h < VEC; h += 4) {
+        const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
+        store_quad<BF, false>(p, at + h, y);
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e)
+    if (e >= skip) store_element<BF>(p, at + e, x[e]);
+}
 
 // Which of up to 256 tensors chunk c belongs to: first[k] is the first chunk of tensor k (first[0] <= c).  Every lane compares its own entries, the
 // bits are counted: one round of loads instead of a chain of them.

@@ -114,7 +114,7 @@ def test_gradient_by_rows(torch, tokens, vocab, cols, kind):
 
 
 @pytest.mark.parametrize("tokens, vocab, cols", [(8192, 300, 20), (8193, 300, 20), (20000, 70000, 20), (40000, 1000, 300), (70001, 32000, 20), (5000, (1 << 21) + 5, 2),
-                                                 (9000, 1 << 22, 2), (600001, 5000, 1), (12000, 1, 5)])
+                                                 (9000, 1 << 22, 2), (600001, 5000, 1), (12000, 1, 5), (9001, 3000, 521)])
 @pytest.mark.parametrize("kind", ["zipf", "all", "mixed"])
 def test_gradient_of_many_tokens(torch, tokens, vocab, cols, kind):
     """Sums that cross many pieces, ids of up to 22 bits."""
@@ -126,6 +126,8 @@ def test_gradient_of_many_tokens(torch, tokens, vocab, cols, kind):
     total, size, count = ref.embed_gradient(ids, dy.double().cpu().numpy(), vocab, 1.0)
     assert np.all(np.abs(out.double().cpu().numpy() - total) <= ref.embed_bound(total, size, count, False))
     assert torch.equal(lordo.embed_gradient(dev, dy, torch.empty_like(out)), out)
+    low = torch.full((vocab * cols + 1,), 9.0, dtype=torch.bfloat16, device="cuda")
+    assert torch.equal(lordo.embed_gradient(dev, dy, low[1:].view(vocab, cols)), out.bfloat16()) and float(low[0]) == 9.0
     by_rows = lordo.embed_gradient_rows(dev, dy, vocab)
     slot = by_rows.index[:vocab].long()
     assert torch.equal(by_rows.rows[slot[slot >= 0]], out[slot >= 0])
