@@ -367,7 +367,7 @@ typedef struct {
 } lordo_grad;
 
 typedef struct {
-  double  beta1, beta2, eps;     /* as in lordo_hparams: in [0, 1), eps outside the root, 0 or from 2^-126 on */
+  double  beta1, beta2, eps;     /* as in lordo_hparams: in [0, 1), eps outside the root, 0 or from 2^-100 on */
   double  weight_decay;          /* decoupled: W <- W - lr * weight_decay * W, >= 0 */
   int32_t bias_correction;       /* as in lordo_hparams */
   int32_t param_dtype;           /* LORDO_F32 or LORDO_BF16 storage of every W (formed in fp32, rounded to nearest-even once) */

@@ -29,6 +29,33 @@ struct AdamwTensor {
   int64_t off;             // first element in the flat state arrays, a multiple of Q8_BLOCK
   int32_t decay, pad_;
 };
+// Step count and what the next step takes from its bias corrections c_i = 1 - beta_i^(t + 1), kept on the device, so that a recorded step counts its replays:
+//   (u / c1) / (sqrt(v / c2) + eps) = ratio u / (sqrt(v) + eps root),   ratio = sqrt(c2) / c1, root = sqrt(c2).
+struct AdamwStep {
+  int64_t t;
+  float ratio, root;
+  double beta1, beta2;
+  int32_t bias_correction, pad_;
+};
+__device__ inline void adamw_step_write(AdamwStep* s, int64_t t) {
+  double c1 = 1.0, c2 = 1.0;
+  if (s->bias_correction) {
+    c1 = 1.0 - int_pow(s->beta1, t + 1);
+    c2 = 1.0 - int_pow(s->beta2, t + 1);
+  }
+  s->t = t;
+  s->ratio = (float)(sqrt(c2) / c1);
+  s->root = (float)sqrt(c2);
+}
+__global__ void k_adamw_set(AdamwStep* s, double beta1, double beta2, int bias_correction, int64_t t) {
+  s->beta1 = beta1; s->beta2 = beta2; s->bias_correction = bias_correction;
+  adamw_step_write(s, t);
+}
+hipError_t launch_adamw_set(AdamwStep* s, double beta1, double beta2, int bias_correction, int64_t t, hipStream_t stream) {
+  hipLaunchKernelGGL(k_adamw_set, dim3(1), dim3(1), 0, stream, s, beta1, beta2, bias_correction, t);
+  return hipGetLastError();
+}
+
 struct AdamwState {
   float *u, *v;            // moments in fp32, or
   uint8_t *cu, *cv;        // their codes and
@@ -46,10 +73,10 @@ struct AdamwArgs {
   uint8_t kind[GROUP];
   RowsOf rows[GROUP_ROWS];
   int32_t count, advance;                 // advance: the last launch of the step moves its count on
-  float b1, omb1, b2, omb2, eps, lr, wd;
+  float b1, omb1, b2, omb2, eps, lr, lr_wd;
   double b1d, omb1d, b2d, omb2d, scale;
   const float* coef;                      // clip coefficient on the device (null: 1)
-  StepDev* step;
+  AdamwStep* step;
   int32_t* flag;                          // latch of steps left out, and the counters 128 bytes behind it
   const AdamwTensor* tensors;             // of this group
   const int32_t* first;                   // chunks before each
@@ -74,18 +101,15 @@ __device__ __forceinline__ uint32_t q8_mix(uint32_t x) {       // x = step Q8_ST
 }
 constexpr int Q8_NAN = 255;              // exponent of a block that holds an infinity or a NaN (or more than 2^127): all its values are NaN
 
-// Four codes of a thread -> moments (not NaN ones: the callers see to those by the exponent).
+// The value of a code in units of 2^E, as the upper half of a double (the lower is zero); not of NaN blocks, which the callers see to by the exponent.
 template <bool SIGNED>
-__device__ __forceinline__ void q8_decode(uint32_t codes, int exponent, double (&x)[4]) {
-  const int top = 8 * (exponent + 1023 - 127) - (SIGNED ? 127 : 255);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int code = (codes >> (8 * e)) & (SIGNED ? 0x7f : 0xff);
-    uint32_t hi = code ? (uint32_t)(code + top) << 17 : 0;
-    if constexpr (SIGNED) hi |= (codes >> (8 * e) & 0x80) << 24;
-    x[e] = __hiloint2double((int)hi, 0);
-  }
+__device__ __forceinline__ uint32_t q8_value(uint32_t code) {
+  const uint32_t c = SIGNED ? code & 0x7f : code;
+  const uint32_t hi = c ? (c - (SIGNED ? 127 : 255) + 8 * 1023) << 17 : 0;
+  return SIGNED ? hi | (code & 0x80) << 24 : hi;
 }
+// 2^E of a block, or NaN
+__device__ __forceinline__ double q8_unit(int exponent) { return __hiloint2double(exponent == Q8_NAN ? 0x7ff80000 : (exponent - 127 + 1023) << 20, 0); }
 
 // Largest of 32 lanes, by the bits of magnitudes: integers order a NaN above everything, so it is not lost.
 template <int CTRL>
@@ -113,7 +137,7 @@ __device__ __forceinline__ uint32_t q8_encode(const double (&x)[4], const float 
   for (int e = 0; e < 4; ++e) most = max(most, __float_as_uint(x32[e]) & (SIGNED ? 0x7fffffffu : 0xffffffffu));
   exponent = q8_exponent(max32(most));
   const int top = 8 * (exponent + 1023 - 127) - (SIGNED ? 127 : 255);
-  const uint32_t some = exponent == 0 ? 0 : SIGNED ? 0x7f : 0xff;               // nothing that fp32 holds: zeros
+  const uint32_t some = exponent == 0 ? 0 : SIGNED ? 0x7f7f7f7fu : 0xffffffffu;  // nothing that fp32 holds: zeros
   int code[4];
   uint32_t least = 0xffffffffu;
 #pragma unroll
@@ -138,12 +162,11 @@ __device__ __forceinline__ uint32_t q8_encode(const double (&x)[4], const float 
       }
     }
   }
-  uint32_t codes = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    uint32_t c = (uint32_t)code[e] & some;
-    if constexpr (SIGNED) c |= ((uint32_t)__double2hiint(x[e]) >> 24) & 0x80u;
-    codes |= c << (8 * e);
+  // the lowest byte of each, and the signs from the highest bytes of the moments
+  uint32_t codes = __builtin_amdgcn_perm(__builtin_amdgcn_perm(code[3], code[2], 0x0c0c0400), __builtin_amdgcn_perm(code[1], code[0], 0x0c0c0400), 0x05040100) & some;
+  if constexpr (SIGNED) {
+    const uint32_t h01 = __builtin_amdgcn_perm(__double2hiint(x[1]), __double2hiint(x[0]), 0x0c0c0703), h23 = __builtin_amdgcn_perm(__double2hiint(x[3]), __double2hiint(x[2]), 0x0c0c0703);
+    codes |= __builtin_amdgcn_perm(h23, h01, 0x05040100) & 0x80808080u;
   }
   return codes;
 }
@@ -234,37 +257,29 @@ __device__ __forceinline__ void load_step(Quad<Q8>& q, const Chunk& c, uint32_t 
 }
 
 struct StepScalars {
-  float scale, inv_c1, inv_c2, wd;
+  float scale, lr, lr_wd, eps;         // lr ratio, lr wd and eps root (AdamwStep)
   double omb1_scale, omb2_scale2;      // (1 - beta1) s and (1 - beta2) s^2
   uint32_t turn;
 };
 
-// (u / c1) / (sqrt(v / c2) + eps) by the approximate root and reciprocal (one unit in the last place each).  Neither takes subnormal numbers: in a wave that
-// has a root of one, its argument is scaled; a sum with eps is none, as the host refuses an eps there; and with eps = 0 a sum of 0 means no gradient so far.
-__device__ __forceinline__ void updates_of(const float (&u)[4], const float (&v)[4], float inv_c1, float inv_c2, float eps, float (&n)[4]) {
-  float x[4], den[4];
-  uint32_t least = 0xffffffffu;
+// u / (sqrt(v) + eps) by the approximate root and reciprocal (one unit in the last place each).  The root does not take subnormal numbers, and gives 0 or what
+// it should, at most 2^-63: nothing beside an eps from 2^-38 on.  Below that the argument is scaled, and a sum of 0 (eps = 0, no gradient so far) gives 0.
+__device__ __forceinline__ void updates_of(const float (&u)[4], const float (&v)[4], float eps, float (&n)[4]) {
+  if (eps >= 0x1p-38f) {                               // (uniform)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[e] = v[e] * inv_c2;
-    least = min(least, __float_as_uint(x[e]) - 1);     // (a zero is above all)
-    den[e] = __builtin_amdgcn_sqrtf(x[e]) + eps;
-  }
-  if (__any(least < __float_as_uint(0x1p-96f) - 1)) {
+    for (int e = 0; e < 4; ++e) n[e] = u[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e]) + eps);
+  } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (x[e] < 0x1p-96f) den[e] = fmaf(__builtin_amdgcn_sqrtf(x[e] * 0x1p64f), 0x1p-32f, eps);
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) n[e] = u[e] * inv_c1 * __builtin_amdgcn_rcpf(den[e]);
-  if (eps == 0.f) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) n[e] = den[e] == 0.f ? 0.f : n[e];
+    for (int e = 0; e < 4; ++e) {
+      const bool small = v[e] < 0x1p-96f;
+      const float den = fmaf(__builtin_amdgcn_sqrtf(small ? v[e] * 0x1p64f : v[e]), small ? 0x1p-32f : 1.f, eps);
+      n[e] = den == 0.f ? 0.f : u[e] * __builtin_amdgcn_rcpf(den);
+    }
   }
 }
 
 template <bool WBF, bool Q8, bool WHOLE>
-__device__ __forceinline__ void store_step(Quad<Q8>& q, const AdamwArgs& a, const Chunk& c, const StepScalars& s, uint32_t i) {
+__device__ __forceinline__ void store_step(Quad<Q8>& q, const AdamwArgs& a, const Chunk& c, const StepScalars& s, const uint32_t* values, uint32_t i) {
   const int cnt = WHOLE || c.n - (int)i >= 4 ? 4 : c.n > (int)i ? c.n - (int)i : 0;
   float u[4], v[4];
   if constexpr (!Q8) {
@@ -282,15 +297,14 @@ __device__ __forceinline__ void store_step(Quad<Q8>& q, const AdamwArgs& a, cons
     // every product and sum is rounded by itself, so that codes do not depend on which of them a compiler joins
 #pragma clang fp contract(off)
     double du[4], dv[4];
-    q8_decode<true>(q.cu, q.eu, du);
-    q8_decode<false>(q.cv, q.ev, dv);
-    const double nan = __hiloint2double(0x7ff80000, 0), b1 = q.eu == Q8_NAN ? nan : a.b1d, b2 = q.ev == Q8_NAN ? nan : a.b2d;
+    const double b1 = a.b1d * q8_unit(q.eu), b2 = a.b2d * q8_unit(q.ev);
     const uint32_t mix0 = s.turn + (c.element + i) * Q8_ELEMENT;
     uint32_t mix[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const double g = (double)q.g[e], g2 = g * g;
-      const double pu = b1 * du[e], qu = s.omb1_scale * g, pv = b2 * dv[e], qv = s.omb2_scale2 * g2;
+      const double ou = __hiloint2double(values[(q.cu >> (8 * e)) & 0xff], 0), ov = __hiloint2double(values[256 + ((q.cv >> (8 * e)) & 0xff)], 0);
+      const double pu = b1 * ou, qu = s.omb1_scale * g, pv = b2 * ov, qv = s.omb2_scale2 * g2;
       du[e] = WHOLE || e < cnt ? pu + qu : 0.0;
       dv[e] = WHOLE || e < cnt ? pv + qv : 0.0;
       u[e] = (float)du[e]; v[e] = (float)dv[e];
@@ -309,9 +323,9 @@ __device__ __forceinline__ void store_step(Quad<Q8>& q, const AdamwArgs& a, cons
     }
   }
   float n[4];
-  updates_of(u, v, s.inv_c1, s.inv_c2, a.eps, n);
+  updates_of(u, v, s.eps, n);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) q.x[e] = fmaf(-a.lr, fmaf(s.wd, q.x[e], n[e]), q.x[e]);
+  for (int e = 0; e < 4; ++e) q.x[e] = fmaf(-s.lr, n[e], fmaf(-s.lr_wd, q.x[e], q.x[e]));
   if (cnt == 4) store_quad<WBF, true>(c.w, i, q.x);
   else
 #pragma unroll
@@ -333,7 +347,7 @@ __device__ __forceinline__ bool last_workgroup(int32_t* counters) {
 
 constexpr int REPS = (int)(ADAMW_CHUNK / 1024);                 // quads of a thread
 template <bool WBF, bool Q8, int KIND>
-__device__ __forceinline__ void step_chunk(const AdamwArgs& a, const Chunk& c, const StepScalars& s) {
+__device__ __forceinline__ void step_chunk(const AdamwArgs& a, const Chunk& c, const StepScalars& s, const uint32_t* values) {
   // Quads requested together.  fp32 moments: bound by memory, all four of a chunk (embedding and head of a 1B model in us: 1 518, 2 507, 4 497; with
   // chunks of 2048, 2 498).  8 bits: bound by instructions, and with the registers of more of them fewer waves fit (1 1000, 2 1019, 4 1009; all with the export).
   constexpr int AHEAD = Q8 ? 1 : REPS;
@@ -344,19 +358,26 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const Chunk& c, c
 #pragma unroll
       for (int r = 0; r < AHEAD; ++r) load_step<WBF, Q8, true, KIND>(q[r], c, (rep + r) * 1024 + threadIdx.x * 4);
 #pragma unroll
-      for (int r = 0; r < AHEAD; ++r) store_step<WBF, Q8, true>(q[r], a, c, s, (rep + r) * 1024 + threadIdx.x * 4);
+      for (int r = 0; r < AHEAD; ++r) store_step<WBF, Q8, true>(q[r], a, c, s, values, (rep + r) * 1024 + threadIdx.x * 4);
     }
   } else {
     for (int rep = 0; rep < REPS && rep * 1024 < c.n; ++rep) {
       Quad<Q8> q;
       load_step<WBF, Q8, false, KIND>(q, c, rep * 1024 + threadIdx.x * 4);
-      store_step<WBF, Q8, false>(q, a, c, s, rep * 1024 + threadIdx.x * 4);
+      store_step<WBF, Q8, false>(q, a, c, s, values, rep * 1024 + threadIdx.x * 4);
     }
   }
 }
 
 template <bool WBF, bool Q8>
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
+  // what the codes of u and v stand for, read from there at an instruction a code instead of six
+  __shared__ uint32_t values[Q8 ? 512 : 1];
+  if constexpr (Q8) {
+    values[threadIdx.x] = q8_value<true>(threadIdx.x);
+    values[256 + threadIdx.x] = q8_value<false>(threadIdx.x);
+    __syncthreads();
+  }
   const int32_t chunk = a.first[0] + (int32_t)blockIdx.x;
   const int k = find_tensor(a.first, a.count, chunk);
   const AdamwTensor t = a.tensors[k];
@@ -370,8 +391,9 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   s.scale = (float)scale;
   s.omb1_scale = a.omb1d * scale;
   s.omb2_scale2 = a.omb2d * (scale * scale);
-  s.inv_c1 = a.step->next_inv_c1; s.inv_c2 = a.step->next_inv_c2;
-  s.wd = t.decay ? a.wd : 0.f;
+  s.lr = a.lr * a.step->ratio;
+  s.lr_wd = t.decay ? a.lr_wd : 0.f;
+  s.eps = a.eps * a.step->root;
   const int64_t steps = a.step->t;
   s.turn = (uint32_t)(steps + 1) * Q8_STEP;
   const int64_t base = (int64_t)(chunk - a.first[k]) * ADAMW_CHUNK, at = t.off + base;
@@ -390,17 +412,17 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   if (kind & G_ROWS) {
     c.row0 = base / t.cols;
     c.col0 = base - c.row0 * t.cols;
-    if (kind & G_BF16) step_chunk<WBF, Q8, ROWS_BF16>(a, c, s);
-    else step_chunk<WBF, Q8, ROWS_F32>(a, c, s);
+    if (kind & G_BF16) step_chunk<WBF, Q8, ROWS_BF16>(a, c, s, values);
+    else step_chunk<WBF, Q8, ROWS_F32>(a, c, s, values);
   } else if (kind & G_BF16) {
-    step_chunk<WBF, Q8, DENSE_BF16>(a, c, s);
+    step_chunk<WBF, Q8, DENSE_BF16>(a, c, s, values);
   } else {
-    step_chunk<WBF, Q8, DENSE_F32>(a, c, s);
+    step_chunk<WBF, Q8, DENSE_F32>(a, c, s, values);
   }
   if (!a.advance) return;
   // t <- t + 1, once every workgroup has read what belongs to t
   __syncthreads();
-  if (threadIdx.x == 0 && last_workgroup(a.flag + 32)) step_write(a.step, steps + 1);
+  if (threadIdx.x == 0 && last_workgroup(a.flag + 32)) adamw_step_write(a.step, steps + 1);
 }
 
 // TO_STATE: moments <- [u | v], in 8 bits with thresholds of one half (a value of the grid stays itself); else [u | v] <- moments.  What lies
@@ -449,14 +471,12 @@ __global__ __launch_bounds__(256) void k_moments(AdamwState st, const AdamwTenso
     } else if (any) {
       if constexpr (Q8) {
         const int eu = st.eu[(at + i) / Q8_BLOCK], ev = st.ev[(at + i) / Q8_BLOCK];
-        double du[4], dv[4];
-        q8_decode<true>(*reinterpret_cast<const uint32_t*>(st.cu + at + i), eu, du);
-        q8_decode<false>(*reinterpret_cast<const uint32_t*>(st.cv + at + i), ev, dv);
+        const uint32_t cu = *reinterpret_cast<const uint32_t*>(st.cu + at + i), cv = *reinterpret_cast<const uint32_t*>(st.cv + at + i);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (e < cnt) {
-            u[e] = eu == Q8_NAN ? NAN : (float)du[e];
-            v[e] = ev == Q8_NAN ? NAN : (float)dv[e];
+            u[e] = (float)(__hiloint2double(q8_value<true>((cu >> (8 * e)) & 0xff), 0) * q8_unit(eu));
+            v[e] = (float)(__hiloint2double(q8_value<false>((cv >> (8 * e)) & 0xff), 0) * q8_unit(ev));
           }
       } else {
         const f32x4a x = *reinterpret_cast<const f32x4a*>(st.u + at + i), y = *reinterpret_cast<const f32x4a*>(st.v + at + i);
@@ -629,7 +649,7 @@ struct lordo_adamw {
     }
     return s;
   }
-  StepDev* step_dev() const { return reinterpret_cast<StepDev*>(arena + step); }
+  AdamwStep* step_dev() const { return reinterpret_cast<AdamwStep*>(arena + step); }
   bool on_its_device() const {
     int cur = -1;
     return hipGetDevice(&cur) == hipSuccess && cur == device;
@@ -644,7 +664,7 @@ int plan_adamw(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams
   if (!tensors || !hp || n <= 0) return LORDO_EINVAL;
   if (!unit(hp->beta1) || !unit(hp->beta2) || !(hp->eps >= 0) || !std::isfinite(hp->eps) || !(hp->weight_decay >= 0) || !std::isfinite(hp->weight_decay))
     return LORDO_EINVAL;
-  if (hp->eps > 0 && hp->eps < 0x1p-126) return LORDO_EINVAL;           // (see updates_of)
+  if (hp->eps > 0 && hp->eps < 0x1p-100) return LORDO_EINVAL;           // (see updates_of)
   if (hp->bias_correction != 0 && hp->bias_correction != 1) return LORDO_EINVAL;
   if (hp->param_dtype != LORDO_F32 && hp->param_dtype != LORDO_BF16) return LORDO_EINVAL;
   if ((hp->state_dtype != LORDO_F32 && hp->state_dtype != LORDO_Q8) || hp->reserved != 0) return LORDO_EINVAL;
@@ -667,7 +687,7 @@ int plan_adamw(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams
   int64_t at = 0;
   auto take = [&](int64_t bytes) { const int64_t r = at; at += (bytes + 255) & ~int64_t(255); return r; };
   c.flag = take(128 + 128 * (COUNTERS + 1));
-  c.step = take(sizeof(StepDev));
+  c.step = take(sizeof(AdamwStep));
   c.table = take((int64_t)sizeof(AdamwTensor) * n);
   c.prefix = take((int64_t)sizeof(int32_t) * (n + 1));
   if (hp->state_dtype == LORDO_Q8) {
@@ -760,7 +780,7 @@ int lordo_adamw_init(lordo_adamw** out, const lordo_tensor* tensors, int32_t n, 
     ADAMW_CHK(hipMemcpy(c->arena + c->prefix, c->first.data(), sizeof(int32_t) * (n + 1), hipMemcpyHostToDevice), "hipMemcpy");
     ADAMW_CHK(launch_fill_zero(c->arena + c->flag, c->step - c->flag, s), "fill");
     ADAMW_CHK(launch_fill_zero(c->arena + c->u, (int64_t)c->bytes - c->u, s), "fill");
-    ADAMW_CHK(launch_step_set(c->step_dev(), hp->beta1, hp->beta2, hp->bias_correction, 0, s), "k_step_set");
+    ADAMW_CHK(launch_adamw_set(c->step_dev(), hp->beta1, hp->beta2, hp->bias_correction, 0, s), "k_adamw_set");
     ADAMW_CHK(hipStreamSynchronize(s), "hipStreamSynchronize");
     *out = c.release();
     return LORDO_OK;
@@ -779,7 +799,7 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
   if ((reinterpret_cast<uintptr_t>(clip) & 3) != 0) return LORDO_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (c->step_dirty) {
-    ADAMW_CHK(launch_step_set(c->step_dev(), c->hp.beta1, c->hp.beta2, c->hp.bias_correction, c->t, s), "k_step_set");
+    ADAMW_CHK(launch_adamw_set(c->step_dev(), c->hp.beta1, c->hp.beta2, c->hp.bias_correction, c->t, s), "k_adamw_set");
   }
   c->step_dirty = true;         // until the whole step is enqueued: a call that fails below leaves the device count to be set back from `t`
   const float* const coef = clip ? clip + 1 : nullptr;
@@ -787,7 +807,7 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
   a.b1 = (float)c->hp.beta1; a.omb1 = (float)(1.0 - c->hp.beta1);
   a.b2 = (float)c->hp.beta2; a.omb2 = (float)(1.0 - c->hp.beta2);
   a.b1d = c->hp.beta1; a.omb1d = 1.0 - c->hp.beta1; a.b2d = c->hp.beta2; a.omb2d = 1.0 - c->hp.beta2;
-  a.eps = (float)c->hp.eps; a.lr = (float)lr; a.wd = (float)c->hp.weight_decay;
+  a.eps = (float)c->hp.eps; a.lr = (float)lr; a.lr_wd = (float)(lr * c->hp.weight_decay);
   a.scale = grad_scale;
   a.coef = coef;
   a.step = c->step_dev();

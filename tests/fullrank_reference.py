@@ -22,9 +22,11 @@ def adamw(w, u, v, g, t, lr, beta1, beta2, eps, wd, bias_correction=True):
 
 
 def adamw_bounds(w_new, w_old, u_terms, v_new, size, lr, wd, w_bf16):
-    """Largest errors of the fp32 step.  u: its five roundings (beta, 1 - beta, s g, their product, the sum) act on its terms; v: seven (s g counts
-    twice), on a sum of positive terms; the update: those of u, half of those of v and of 1 / c2, the root, eps, 1 / c1, the product and the quotient, below
-    20 in all; W: lr, wd and two sums.  A weight in bf16 is rounded once more; 2^-126 where results are subnormal."""
+    """Largest errors of the fp32 step, in halves of a step.  u: five roundings (beta, 1 - beta, s g, their product, the sum) act on its terms; v: seven (s g
+    counts twice), on a sum of positive terms.  The update lr sqrt(c2) / c1 u / (sqrt(v) + eps sqrt(c2)): 5 of u, 3.5 of v and 2 of its root (one unit), 1 of
+    the sum, 2 of the reciprocal (one unit), 1 of the product, 3 of lr sqrt(c2) / c1: 17.5.  W - lr wd W: 1 of lr wd, and 1 of the result, which is at
+    most the new weight and the update; 1 of the new weight: 20 of the update cover it.  A weight in bf16 is rounded once more; 2^-126 where results are
+    subnormal."""
     tiny = 2.0 ** -126
     bw = EPS32 * (2 * np.abs(w_new) + lr * (20 * size + 4 * wd * np.abs(w_old))) + tiny
     if w_bf16:
