@@ -406,15 +406,20 @@ def _torch():
 
 
 def _same_device(torch, *tensors):
-    """Refuses tensors that are not on the current GPU: the calls without a context enqueue there."""
+    """The current GPU, where all tensors have to be: the calls without a context enqueue there."""
     at = torch.cuda.current_device() if tensors[0].is_cuda else -1
     for t in tensors:
         if t.get_device() != at or at < 0:
             raise ValueError("expected CUDA tensors on the current device, got " + ", ".join(str(t.device) for t in tensors))
+    return at
 
 
-def _stream_of(torch):
-    return torch.cuda.current_stream().cuda_stream
+def _stream_of(torch, at=None):
+    """Address of the current stream of GPU `at` (the current one).  torch's own look-up takes 0.1 us, the Stream object of its public call 2.6."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        return torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device() if at is None else at)
 
 
 def _float_code(t, torch):
@@ -485,7 +490,8 @@ def grad_norm(grads, max_norm=float("inf"), out=None):
     torch = _torch()
     if not isinstance(grads, GradList):
         grads = GradList(grads)
-    if grads.at != torch.cuda.current_device():
+    gpu = torch.cuda.current_device()
+    if grads.at != gpu:
         raise ValueError(f"tensors are on {grads.device}, which is not the current device")
     # the result and, from 256 bytes on, the workspace in one allocation
     room = torch.empty(64 + NORM_WORKSPACE_BYTES // 4, dtype=torch.float32, device=grads.device)
@@ -494,7 +500,7 @@ def grad_norm(grads, max_norm=float("inf"), out=None):
         out = room[:2]
     elif out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous() or out.device != grads.device:
         raise ValueError("expected a contiguous float32 tensor of two elements on the gradients' device")
-    _check(load().lordo_grad_norm(grads.arr, len(grads.grads), max_norm, out.data_ptr(), at + 256, NORM_WORKSPACE_BYTES, _stream_of(torch)))
+    _check(load().lordo_grad_norm(grads.arr, len(grads.grads), max_norm, out.data_ptr(), at + 256, NORM_WORKSPACE_BYTES, _stream_of(torch, gpu)))
     return out
 
 
@@ -624,9 +630,9 @@ def embed_lookup(table, ids, scale=1.0, out=None, dtype=None):
         out = torch.empty((*ids.shape, cols), dtype=dtype or table.dtype, device=table.device)
     elif tuple(out.shape) != (*ids.shape, cols) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"expected a contiguous output of shape {(*ids.shape, cols)}")
-    _same_device(torch, table, ids, out)
+    at = _same_device(torch, table, ids, out)
     _check(load().lordo_embed_lookup(table.data_ptr(), _float_code(table, torch), vocab, cols, p, code, n, scale, out.data_ptr(),
-                                     _float_code(out, torch), _stream_of(torch)))
+                                     _float_code(out, torch), _stream_of(torch, at)))
     return out
 
 
@@ -645,22 +651,22 @@ def embed_gradient(ids, dy, out, scale=1.0, pad_id=-1, accumulate=False):
     torch = _torch()
     if out.dim() != 2 or not out.is_contiguous() or dy.shape[-1] != out.shape[1]:
         raise ValueError("expected a contiguous (vocab, cols) output")
-    _same_device(torch, ids, dy, out)
+    at = _same_device(torch, ids, dy, out)
     p, code, n = _ids(ids, torch)
     cols, size, ws = _workspace(ids, dy, out.shape[0], torch)
     _check(load().lordo_embed_gradient(p, code, n, dy.data_ptr(), _float_code(dy, torch), out.shape[0], cols, scale, pad_id, int(accumulate),
-                                       out.data_ptr(), _float_code(out, torch), ws.data_ptr(), size, _stream_of(torch)))
+                                       out.data_ptr(), _float_code(out, torch), ws.data_ptr(), size, _stream_of(torch, at)))
     return out
 
 
 def embed_gradient_rows(ids, dy, vocab, scale=1.0, pad_id=-1, dtype=None) -> RowGrad:
     """Gradient of embed_lookup by rows, for AdamW.local_step and grad_norm: one row per different token, of `dtype` (float32 if None)."""
     torch = _torch()
-    _same_device(torch, ids, dy)
+    at = _same_device(torch, ids, dy)
     p, code, n = _ids(ids, torch)
     cols, size, ws = _workspace(ids, dy, vocab, torch)
     rows = torch.empty((n, cols), dtype=dtype or torch.float32, device=dy.device)
     index = torch.empty(vocab + n, dtype=torch.int32, device=dy.device)
     _check(load().lordo_embed_gradient_rows(p, code, n, dy.data_ptr(), _float_code(dy, torch), vocab, cols, scale, pad_id, rows.data_ptr(),
-                                            _float_code(rows, torch), index.data_ptr(), ws.data_ptr(), size, _stream_of(torch)))
+                                            _float_code(rows, torch), index.data_ptr(), ws.data_ptr(), size, _stream_of(torch, at)))
     return RowGrad(rows, index, vocab)
