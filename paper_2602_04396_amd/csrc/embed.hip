@@ -322,6 +322,15 @@ __global__ __launch_bounds__(1024) void k_join_tiles(Sorted in, int32_t tokens, 
   if (id == vocab || beyond != id || before == id) return;
   __shared__ float sums[4][1024];
   const int lane = threadIdx.x & 63, group = threadIdx.x >> 8, column = (threadIdx.x & 255) * 4;
+  const int64_t c = (int64_t)blockIdx.y * 1024 + column;
+  const int cnt = cols - c >= 4 ? 4 : cols > c ? (int)(cols - c) : 0;
+  const int32_t own = lane < tile_tokens ? in.key[first + lane] : id;
+  float old[4] = {0.f, 0.f, 0.f, 0.f};                 // what the output holds, requested with what follows
+  if (o.add && group == 0) {
+    if (cnt == 4) load_quad<OUT_BF, false>(o.dst, (int64_t)id * cols + c, old);
+    else
+      for (int e = 0; e < cnt; ++e) old[e] = load_element<OUT_BF>(o.dst, (int64_t)id * cols + c + e);
+  }
   int32_t last = tile + 2;                             // last tile that begins with the run
   for (bool more = true; more;) {
     const int32_t k = last + 1 + lane;
@@ -329,12 +338,9 @@ __global__ __launch_bounds__(1024) void k_join_tiles(Sorted in, int32_t tokens, 
     last += same == ~0ull ? 64 : __ffsll((unsigned long long)~same) - 1;
     more = same == ~0ull;
   }
-  const int32_t own = lane < tile_tokens ? in.key[first + lane] : id;
   const uint64_t other = __ballot(own != id);
   const int start = other ? 64 - __clzll((long long)other) : 0;
   const int32_t each = (last - tile + 3) / 4, from = tile + 1 + group * each, to = std::min(from + each, last + 1);
-  const int64_t c = (int64_t)blockIdx.y * 1024 + column;
-  const int cnt = cols - c >= 4 ? 4 : cols > c ? (int)(cols - c) : 0;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   const float* const p = o.part + c;
   if (group == 0)
@@ -359,12 +365,11 @@ __global__ __launch_bounds__(1024) void k_join_tiles(Sorted in, int32_t tokens, 
   if (group != 0 || cnt == 0) return;
   const int64_t at = (int64_t)(o.index ? first + start : id) * cols + c;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) sum[e] = (((sum[e] + sums[1][column + e]) + sums[2][column + e]) + sums[3][column + e]) * o.scale;
-  for (int e = 0; e < cnt; ++e) {
-    if (o.add) sum[e] += load_element<OUT_BF>(o.dst, at + e);
-    if (cnt < 4) store_element<OUT_BF>(o.dst, at + e, sum[e]);
-  }
-  if (cnt == 4) store_quad<OUT_BF, false>(o.dst, at, sum);
+  for (int e = 0; e < 4; ++e) sum[e] = (((sum[e] + sums[1][column + e]) + sums[2][column + e]) + sums[3][column + e]) * o.scale + old[e];
+  if (cnt < 4)
+    for (int e = 0; e < cnt; ++e) store_element<OUT_BF>(o.dst, at + e, sum[e]);
+  else
+    store_quad<OUT_BF, false>(o.dst, at, sum);
 }
 
 }  // namespace lordo

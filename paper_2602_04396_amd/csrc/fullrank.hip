@@ -14,7 +14,8 @@
 
 namespace lordo {
 
-constexpr int64_t ADAMW_CHUNK = 4096;    // elements of one tensor that a workgroup takes
+// Elements of one tensor that a workgroup takes: 4096, or 1024 where those would be less than 1024 workgroups (four a compute unit).
+constexpr int64_t ADAMW_CHUNK = 4096, ADAMW_SMALL_CHUNK = 1024, ADAMW_MANY = 1024;
 constexpr int Q8_BLOCK = 128;            // elements that share a scale
 constexpr int GROUP = 200;               // tensors of one launch, and gradients by rows among them: their pointers travel in the kernel arguments (below 4 KiB)
 constexpr int GROUP_ROWS = 8;
@@ -34,22 +35,19 @@ struct AdamwTensor {
 struct AdamwStep {
   int64_t t;
   float ratio, root;
-  double beta1, beta2;
-  int32_t bias_correction, pad_;
 };
-__device__ inline void adamw_step_write(AdamwStep* s, int64_t t) {
+__device__ inline void adamw_step_write(AdamwStep* s, int64_t t, double beta1, double beta2, int bias_correction) {
   double c1 = 1.0, c2 = 1.0;
-  if (s->bias_correction) {
-    c1 = 1.0 - int_pow(s->beta1, t + 1);
-    c2 = 1.0 - int_pow(s->beta2, t + 1);
+  if (bias_correction) {
+    c1 = 1.0 - int_pow(beta1, t + 1);
+    c2 = 1.0 - int_pow(beta2, t + 1);
   }
   s->t = t;
   s->ratio = (float)(sqrt(c2) / c1);
   s->root = (float)sqrt(c2);
 }
 __global__ void k_adamw_set(AdamwStep* s, double beta1, double beta2, int bias_correction, int64_t t) {
-  s->beta1 = beta1; s->beta2 = beta2; s->bias_correction = bias_correction;
-  adamw_step_write(s, t);
+  adamw_step_write(s, t, beta1, beta2, bias_correction);
 }
 hipError_t launch_adamw_set(AdamwStep* s, double beta1, double beta2, int bias_correction, int64_t t, hipStream_t stream) {
   hipLaunchKernelGGL(k_adamw_set, dim3(1), dim3(1), 0, stream, s, beta1, beta2, bias_correction, t);
@@ -72,7 +70,7 @@ struct AdamwArgs {
   const void* g[GROUP];
   uint8_t kind[GROUP];
   RowsOf rows[GROUP_ROWS];
-  int32_t count, advance;                 // advance: the last launch of the step moves its count on
+  int32_t count, advance, bias_correction; // advance: the last launch of the step moves its count on
   float b1, omb1, b2, omb2, eps, lr, lr_wd;
   double b1d, omb1d, b2d, omb2d, scale;
   const float* coef;                      // clip coefficient on the device (null: 1)
@@ -336,22 +334,25 @@ __device__ __forceinline__ void store_step(Quad<Q8>& q, const AdamwArgs& a, cons
 // The workgroup that is the last of its launch to come here.  Counters for a sixteenth of the workgroups each, so that few wait for one address; the last of each
 // counts on the one behind them, and every counter is left at zero.
 __device__ __forceinline__ bool last_workgroup(int32_t* counters) {
+  if (gridDim.x <= 64) {                               // few: one counter
+    if (atomicAdd(counters, 1) != (int32_t)gridDim.x - 1) return false;
+    atomicExch(counters, 0);
+    return true;
+  }
   const int32_t k = (int32_t)blockIdx.x % COUNTERS, all = ((int32_t)gridDim.x - k + COUNTERS - 1) / COUNTERS;
   if (atomicAdd(counters + 32 * k, 1) != all - 1) return false;
   atomicExch(counters + 32 * k, 0);
-  const int32_t used = (int32_t)gridDim.x < COUNTERS ? (int32_t)gridDim.x : COUNTERS;
-  if (atomicAdd(counters + 32 * COUNTERS, 1) != used - 1) return false;
+  if (atomicAdd(counters + 32 * COUNTERS, 1) != COUNTERS - 1) return false;
   atomicExch(counters + 32 * COUNTERS, 0);
   return true;
 }
 
-constexpr int REPS = (int)(ADAMW_CHUNK / 1024);                 // quads of a thread
-template <bool WBF, bool Q8, int KIND>
+template <bool WBF, bool Q8, int64_t CHUNK, int KIND>
 __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const Chunk& c, const StepScalars& s, const uint32_t* values) {
   // Quads requested together.  fp32 moments: bound by memory, all four of a chunk (embedding and head of a 1B model in us: 1 518, 2 507, 4 497; with
   // chunks of 2048, 2 498).  8 bits: bound by instructions, and with the registers of more of them fewer waves fit (1 1000, 2 1019, 4 1009; all with the export).
-  constexpr int AHEAD = Q8 ? 1 : REPS;
-  if (c.n == ADAMW_CHUNK) {
+  constexpr int REPS = (int)(CHUNK / 1024), AHEAD = Q8 ? 1 : REPS;
+  if (c.n == CHUNK) {
 #pragma unroll
     for (int rep = 0; rep < REPS; rep += AHEAD) {
       Quad<Q8> q[AHEAD];
@@ -369,7 +370,7 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const Chunk& c, c
   }
 }
 
-template <bool WBF, bool Q8>
+template <bool WBF, bool Q8, int64_t CHUNK>
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   // what the codes of u and v stand for, read from there at an instruction a code instead of six
   __shared__ uint32_t values[Q8 ? 512 : 1];
@@ -396,7 +397,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   s.eps = a.eps * a.step->root;
   const int64_t steps = a.step->t;
   s.turn = (uint32_t)(steps + 1) * Q8_STEP;
-  const int64_t base = (int64_t)(chunk - a.first[k]) * ADAMW_CHUNK, at = t.off + base;
+  const int64_t base = (int64_t)(chunk - a.first[k]) * CHUNK, at = t.off + base;
   const uint8_t kind = a.kind[k];
   const int dense = kind & G_ROWS ? 0 : kind & G_BF16 ? 2 : 4;         // bytes of an element of a dense gradient
   Chunk c;
@@ -407,36 +408,37 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   c.cu = a.st.cu + at; c.cv = a.st.cv + at;
   c.eu = a.st.eu + at / Q8_BLOCK; c.ev = a.st.ev + at / Q8_BLOCK;
   c.cols = t.cols; c.row0 = c.col0 = 0;
-  c.n = (int32_t)std::min(t.n - base, ADAMW_CHUNK);
+  c.n = (int32_t)std::min(t.n - base, CHUNK);
   c.element = (uint32_t)base;
   if (kind & G_ROWS) {
     c.row0 = base / t.cols;
     c.col0 = base - c.row0 * t.cols;
-    if (kind & G_BF16) step_chunk<WBF, Q8, ROWS_BF16>(a, c, s, values);
-    else step_chunk<WBF, Q8, ROWS_F32>(a, c, s, values);
+    if (kind & G_BF16) step_chunk<WBF, Q8, CHUNK, ROWS_BF16>(a, c, s, values);
+    else step_chunk<WBF, Q8, CHUNK, ROWS_F32>(a, c, s, values);
   } else if (kind & G_BF16) {
-    step_chunk<WBF, Q8, DENSE_BF16>(a, c, s, values);
+    step_chunk<WBF, Q8, CHUNK, DENSE_BF16>(a, c, s, values);
   } else {
-    step_chunk<WBF, Q8, DENSE_F32>(a, c, s, values);
+    step_chunk<WBF, Q8, CHUNK, DENSE_F32>(a, c, s, values);
   }
   if (!a.advance) return;
   // t <- t + 1, once every workgroup has read what belongs to t
   __syncthreads();
-  if (threadIdx.x == 0 && last_workgroup(a.flag + 32)) adamw_step_write(a.step, steps + 1);
+  if (threadIdx.x == 0 && last_workgroup(a.flag + 32)) adamw_step_write(a.step, steps + 1, a.b1d, a.b2d, a.bias_correction);
 }
 
 // TO_STATE: moments <- [u | v], in 8 bits with thresholds of one half (a value of the grid stays itself); else [u | v] <- moments.  What lies
 // between the tensors is written as zero.
 template <bool Q8, bool TO_STATE>
-__global__ __launch_bounds__(256) void k_moments(AdamwState st, const AdamwTensor* tensors, const int32_t* first, int32_t count, float* plain, int64_t total) {
+__global__ __launch_bounds__(256) void k_moments(AdamwState st, const AdamwTensor* tensors, const int32_t* first, int32_t count, int32_t chunk_elements, float* plain,
+                                                 int64_t total) {
   const int32_t chunk = first[0] + (int32_t)blockIdx.x;
   const int k = find_tensor(first, count, chunk);
   const AdamwTensor t = tensors[k];
-  const int64_t base = (int64_t)(chunk - first[k]) * ADAMW_CHUNK, at = t.off + base;
-  const int32_t n = (int32_t)std::min(t.n - base, ADAMW_CHUNK), padded = (n + Q8_BLOCK - 1) / Q8_BLOCK * Q8_BLOCK;
+  const int64_t base = (int64_t)(chunk - first[k]) * chunk_elements, at = t.off + base;
+  const int32_t n = (int32_t)std::min<int64_t>(t.n - base, chunk_elements), padded = (n + Q8_BLOCK - 1) / Q8_BLOCK * Q8_BLOCK;
   float* const pu = plain + at;
   float* const pv = plain + total + at;
-  for (int rep = 0; rep < REPS && rep * 1024 < padded; ++rep) {
+  for (int rep = 0; rep * 1024 < padded; ++rep) {
     const int i = rep * 1024 + (int)threadIdx.x * 4, cnt = std::min(std::max(n - i, 0), 4);
     const bool any = i < padded;
     float u[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -553,9 +555,21 @@ __device__ __forceinline__ double chunk_squares(const void* g, int64_t base, int
     }
   return sum[0] + sum[1];
 }
-// The same of a gradient by rows: rows that belong to no row of the tensor hold nothing.
+// The same of a gradient by rows: rows that belong to no row of the tensor hold nothing.  Long rows are taken one by one, so that whether a row is there is
+// asked once; of short ones each thread asks for its own.
 template <bool BF>
 __device__ __forceinline__ double chunk_squares_of_rows(const void* g, const int32_t* owner, int64_t cols, int64_t base, int64_t n, int threads) {
+  if (cols >= 1024) {
+    double sum = 0.0;
+    const int64_t end = std::min(base + NORM_CHUNK, n);
+    int64_t row = base / cols;
+    for (int64_t at = base; at < end; ++row) {
+      const int64_t to = std::min((row + 1) * cols, end);
+      if (owner[row] >= 0) sum += chunk_squares<BF>(g, at, to, threads);
+      at = to;
+    }
+    return sum;
+  }
   double sum = 0.0;
   const int64_t end = std::min(base + NORM_CHUNK, n), row0 = base / cols, col0 = base - row0 * cols;
   for (int64_t i = base + (int64_t)threadIdx.x * 4; i < end; i += (int64_t)threads * 4) {
@@ -632,6 +646,7 @@ struct lordo_adamw {
   std::vector<AdamwTensor> tensors;
   std::vector<int32_t> first;            // chunks before each tensor; the total at the end
   int64_t total = 0;                     // elements of a flat state array
+  int64_t chunk = ADAMW_CHUNK;           // elements of a workgroup
   size_t bytes = 0;
   int64_t flag = 0, step = 0, table = 0, prefix = 0, u = 0, v = 0, eu = 0, ev = 0;     // byte offsets in the arena
   char* arena = nullptr;
@@ -674,13 +689,19 @@ int plan_adamw(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams
     const lordo_tensor& s = tensors[i];
     if (s.rows <= 0 || s.cols <= 0 || s.rows > (int64_t(1) << 38) || s.cols > (int64_t(1) << 38) / s.rows) return LORDO_EINVAL;
     if ((s.decay != 0 && s.decay != 1) || s.reserved != 0) return LORDO_EINVAL;
+    chunks += (s.rows * s.cols + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+    if (chunks > (int64_t(1) << 30)) return LORDO_EINVAL;
+  }
+  c.chunk = chunks >= ADAMW_MANY ? ADAMW_CHUNK : ADAMW_SMALL_CHUNK;
+  chunks = 0;
+  for (int i = 0; i < n; ++i) {
+    const lordo_tensor& s = tensors[i];
     AdamwTensor t{};
     t.n = s.rows * s.cols; t.cols = s.cols; t.off = c.total; t.decay = s.decay;
     c.first.push_back((int32_t)chunks);
     c.tensors.push_back(t);
     c.total += (t.n + Q8_BLOCK - 1) / Q8_BLOCK * Q8_BLOCK;
-    chunks += (t.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
-    if (chunks > (int64_t(1) << 30)) return LORDO_EINVAL;
+    chunks += (t.n + c.chunk - 1) / c.chunk;
   }
   c.first.push_back((int32_t)chunks);
   c.shapes.assign(tensors, tensors + n);
@@ -712,6 +733,12 @@ bool good_grad(const lordo_grad& g) {
   return (reinterpret_cast<uintptr_t>(g.data) & (g.dtype == LORDO_F32 ? 3 : 1)) == 0 && (reinterpret_cast<uintptr_t>(g.index) & 3) == 0;
 }
 
+template <bool Q8, int64_t CHUNK>
+void launch_step(bool w_bf16, dim3 grid, hipStream_t s, const AdamwArgs& a) {
+  if (w_bf16) hipLaunchKernelGGL((k_adamw<true, Q8, CHUNK>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_adamw<false, Q8, CHUNK>), grid, dim3(256), 0, s, a);
+}
+
 uint8_t grad_kind(const lordo_grad& g, int rows) { return (uint8_t)((g.dtype == LORDO_BF16 ? G_BF16 : 0) | (g.index ? G_ROWS | rows << 2 : 0)); }
 
 #define ADAMW_CHK(expr, what)                                                                     \
@@ -732,11 +759,11 @@ int moments(lordo_adamw* c, float* plain, bool to_state, hipStream_t s) {
     const int count = std::min(256, n - at);
     const dim3 grid((unsigned)(c->first[at + count] - c->first[at])), block(256);
     if (c->hp.state_dtype == LORDO_Q8) {
-      if (to_state) hipLaunchKernelGGL((k_moments<true, true>), grid, block, 0, s, st, tensors, first, count, plain, c->total);
-      else hipLaunchKernelGGL((k_moments<true, false>), grid, block, 0, s, st, tensors, first, count, plain, c->total);
+      if (to_state) hipLaunchKernelGGL((k_moments<true, true>), grid, block, 0, s, st, tensors, first, count, (int32_t)c->chunk, plain, c->total);
+      else hipLaunchKernelGGL((k_moments<true, false>), grid, block, 0, s, st, tensors, first, count, (int32_t)c->chunk, plain, c->total);
     } else {
-      if (to_state) hipLaunchKernelGGL((k_moments<false, true>), grid, block, 0, s, st, tensors, first, count, plain, c->total);
-      else hipLaunchKernelGGL((k_moments<false, false>), grid, block, 0, s, st, tensors, first, count, plain, c->total);
+      if (to_state) hipLaunchKernelGGL((k_moments<false, true>), grid, block, 0, s, st, tensors, first, count, (int32_t)c->chunk, plain, c->total);
+      else hipLaunchKernelGGL((k_moments<false, false>), grid, block, 0, s, st, tensors, first, count, (int32_t)c->chunk, plain, c->total);
     }
     const int rc = launched("k_moments");
     if (rc != LORDO_OK) return rc;
@@ -813,6 +840,7 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
   a.step = c->step_dev();
   a.st = c->state();
   a.flag = reinterpret_cast<int32_t*>(c->arena + c->flag);
+  a.bias_correction = c->hp.bias_correction;
   for (int at = 0; at < n;) {
     a.count = 0;
     for (int rows = 0; at + a.count < n && a.count < GROUP; ++a.count) {
@@ -825,17 +853,13 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
     }
     a.tensors = reinterpret_cast<const AdamwTensor*>(c->arena + c->table) + at;
     a.first = reinterpret_cast<const int32_t*>(c->arena + c->prefix) + at;
-    const dim3 grid((unsigned)(c->first[at + a.count] - c->first[at])), block(256);
+    const dim3 grid((unsigned)(c->first[at + a.count] - c->first[at]));
     at += a.count;
     a.advance = at == n;
     const bool bf = c->hp.param_dtype == LORDO_BF16;
-    if (c->hp.state_dtype == LORDO_Q8) {
-      if (bf) hipLaunchKernelGGL((k_adamw<true, true>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((k_adamw<false, true>), grid, block, 0, s, a);
-    } else {
-      if (bf) hipLaunchKernelGGL((k_adamw<true, false>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((k_adamw<false, false>), grid, block, 0, s, a);
-    }
+    const bool small = c->chunk == ADAMW_SMALL_CHUNK;
+    if (c->hp.state_dtype == LORDO_Q8) small ? launch_step<true, ADAMW_SMALL_CHUNK>(bf, grid, s, a) : launch_step<true, ADAMW_CHUNK>(bf, grid, s, a);
+    else small ? launch_step<false, ADAMW_SMALL_CHUNK>(bf, grid, s, a) : launch_step<false, ADAMW_CHUNK>(bf, grid, s, a);
     const int rc = launched("k_adamw");
     if (rc != LORDO_OK) return rc;
   }
