@@ -140,7 +140,7 @@ __device__ __forceinline__ uint32_t q8_encode(const double (&x)[4], const float 
   uint32_t least = 0xffffffffu;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const uint32_t m = (uint32_t)__double2hiint(x[e]) & 0x7fffffffu;
+    const uint32_t m = (uint32_t)__double2hiint(x[e]) & (SIGNED ? 0x7fffffffu : 0xffffffffu);
     code[e] = (int)((m + w(e)) >> 17) - top;           // far below 0 for a zero
     if constexpr (SIGNED) {
       code[e] = max(code[e], 0);
