@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "lib", "liblordo.so")
@@ -449,32 +450,38 @@ class RowGrad:
         return (self.vocab, self.rows.shape[1])
 
 
+_float_codes = {}
+
+
 class GradList:
     """A list of gradients (tensors of one or two dimensions, RowGrads) validated once, reusable across calls; keeps them alive."""
 
     def __init__(self, grads):
-        torch = _torch()
-        self.grads = list(grads)
-        if not self.grads:
+        codes = _float_codes
+        if not codes:
+            torch = _torch()
+            codes.update({torch.float32: F32, torch.bfloat16: BF16})
+        self.grads = grads = list(grads)
+        if not grads:
             raise ValueError("no gradients")
-        self.arr = (Grad * len(self.grads))()
-        flat = []
-        for a, g in zip(self.arr, self.grads):
-            if isinstance(g, RowGrad):
-                data, a.index, a.slots = g.rows, g.index.data_ptr(), g.rows.shape[0]
-                flat.append(g.index)
-                if not g.index.is_contiguous():
-                    raise ValueError("expected contiguous gradients")
+        first = grads[0].rows if type(grads[0]) is RowGrad else grads[0]
+        self.at, self.device = at, _ = first.get_device(), first.device
+        fields = []
+        for g in grads:
+            index = slots = 0
+            if type(g) is RowGrad:
+                index, slots, vocab, same = g.index.data_ptr(), len(g.rows), g.vocab, g.index.get_device() == at and g.index.is_contiguous()
+                g = g.rows
+                rows, cols = vocab, g.shape[1]
             else:
-                data = g
-            a.rows, a.cols = g.shape if isinstance(g, RowGrad) else _rows_cols(g)
-            a.data, a.dtype = data.data_ptr() or None, _float_code(data, torch)
-            if not data.is_contiguous():
-                raise ValueError("expected contiguous gradients")
-            flat.append(data)
-        self.device, self.at = flat[0].device, flat[0].get_device()
-        if self.at < 0 or any(t.get_device() != self.at for t in flat):
-            raise ValueError("expected CUDA tensors on one device")
+                same = True
+                shape = g.shape
+                rows, cols = shape if len(shape) == 2 else (1, g.numel())
+            code = codes.get(g.dtype)
+            if code is None or not g.is_contiguous() or not same or g.get_device() != at or at < 0:
+                raise ValueError(f"expected contiguous float32 or bfloat16 CUDA tensors on one device, got {g.dtype} on {g.device}")
+            fields += (g.data_ptr(), index, rows, cols, slots, code, 0)
+        self.arr = (Grad * len(grads)).from_buffer_copy(struct.pack("QQqqqii" * len(grads), *fields))
 
     def __len__(self):
         return len(self.grads)
@@ -659,14 +666,22 @@ def embed_gradient(ids, dy, out, scale=1.0, pad_id=-1, accumulate=False):
     return out
 
 
-def embed_gradient_rows(ids, dy, vocab, scale=1.0, pad_id=-1, dtype=None) -> RowGrad:
-    """Gradient of embed_lookup by rows, for AdamW.local_step and grad_norm: one row per different token, of `dtype` (float32 if None)."""
+def embed_gradient_rows(ids, dy, vocab, scale=1.0, pad_id=-1, dtype=None, out=None) -> RowGrad:
+    """Gradient of embed_lookup by rows, for AdamW.local_step and grad_norm: one row per different token, of `dtype` (float32 if None).  `out`: an
+    earlier result for as many tokens to write over, so that a GradList that holds it stays good."""
     torch = _torch()
     at = _same_device(torch, ids, dy)
     p, code, n = _ids(ids, torch)
     cols, size, ws = _workspace(ids, dy, vocab, torch)
-    rows = torch.empty((n, cols), dtype=dtype or torch.float32, device=dy.device)
-    index = torch.empty(vocab + n, dtype=torch.int32, device=dy.device)
+    if out is None:
+        rows = torch.empty((n, cols), dtype=dtype or torch.float32, device=dy.device)
+        index = torch.empty(vocab + n, dtype=torch.int32, device=dy.device)
+        out = RowGrad(rows, index, vocab)
+    else:
+        rows, index = out.rows, out.index
+        if out.vocab != vocab or rows.shape != (n, cols) or (dtype is not None and rows.dtype != dtype) or not rows.is_contiguous() or not index.is_contiguous():
+            raise ValueError(f"expected a RowGrad of {n} rows of {cols} for {vocab} ids")
+        _same_device(torch, rows, index)
     _check(load().lordo_embed_gradient_rows(p, code, n, dy.data_ptr(), _float_code(dy, torch), vocab, cols, scale, pad_id, rows.data_ptr(),
                                             _float_code(rows, torch), index.data_ptr(), ws.data_ptr(), size, _stream_of(torch, at)))
-    return RowGrad(rows, index, vocab)
+    return out

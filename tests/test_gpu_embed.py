@@ -111,6 +111,10 @@ def test_gradient_by_rows(torch, tokens, vocab, cols, kind):
         assert np.array_equal(owner[slot[there]], there)
         assert torch.equal(by_rows.rows[torch.tensor(slot[there]).cuda().long()], dense[torch.tensor(there).cuda().long()].to(dtype))
         assert by_rows.shape == (vocab, cols)
+        again = lordo.RowGrad(torch.full_like(by_rows.rows, 7.0), torch.zeros_like(by_rows.index), vocab)      # rows of no id stay as they were
+        assert lordo.embed_gradient_rows(ids, dy, vocab, scale=0.7, out=again) is again and torch.equal(again.index, by_rows.index)
+        held = by_rows.index[vocab:] >= 0
+        assert torch.equal(again.rows[held], by_rows.rows[held]) and torch.all(again.rows[~held] == 7.0)
 
 
 @pytest.mark.parametrize("tokens, vocab, cols", [(8192, 300, 20), (8193, 300, 20), (20000, 70000, 20), (40000, 1000, 300), (70001, 32000, 20), (5000, (1 << 21) + 5, 2),
@@ -140,7 +144,8 @@ def test_refusals(torch):
                  lambda: lordo.embed_lookup(table, ids, out=torch.zeros(3, 5, device="cuda")), lambda: lordo.embed_lookup(table, ids.cpu()),
                  lambda: lordo.embed_gradient(ids, dy[:2], table), lambda: lordo.embed_gradient(ids, dy, table.t()),
                  lambda: lordo.embed_gradient(ids, dy, torch.zeros(8, 5, device="cuda")), lambda: lordo.embed_gradient(ids, dy.t().contiguous().t(), table),
-                 lambda: lordo.embed_gradient_rows(ids, dy.cpu(), 8)):
+                 lambda: lordo.embed_gradient_rows(ids, dy.cpu(), 8), lambda: lordo.embed_gradient_rows(ids, dy, 8, out=lordo.embed_gradient_rows(ids, dy, 9)),
+                 lambda: lordo.embed_gradient_rows(ids, dy, 8, out=lordo.embed_gradient_rows(ids[:2], dy[:2], 8))):
         with pytest.raises(ValueError):
             call()
     with pytest.raises(lordo.LordoError):
