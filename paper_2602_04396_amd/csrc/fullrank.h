@@ -82,6 +82,7 @@ struct Piece<false, 4> {
 template <>
 struct Piece<true, 4> {
   u32x2u v;
+  __device__ __forceinline__ void clear() { v = u32x2u{0, 0}; }
   __device__ __forceinline__ void load(const void* p, int64_t at) { v = *reinterpret_cast<const u32x2u*>(reinterpret_cast<const uint16_t*>(p) + at); }
   __device__ __forceinline__ float value(int e) const { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
 };

@@ -19,9 +19,10 @@ constexpr int64_t ADAMW_CHUNK = 4096, ADAMW_SMALL_CHUNK = 1024, ADAMW_MANY = 102
 constexpr int Q8_BLOCK = 128;            // elements that share a scale
 constexpr int GROUP = 200;               // tensors of one launch, and gradients by rows among them: their pointers travel in the kernel arguments (below 4 KiB)
 constexpr int GROUP_ROWS = 8;
-constexpr int64_t NORM_CHUNK = 16384;
+// Elements of a workgroup of the norm at a time: 16384, or 2048 where those would be less than one for each of its 1024 workgroups.
+constexpr int64_t NORM_CHUNK = 16384, NORM_SMALL_CHUNK = 2048;
 constexpr int NORM_BLOCKS = 1024;
-constexpr int NORM_ALONE = 6;           // chunks that one workgroup takes without a second launch
+constexpr int64_t NORM_ALONE = 98304;    // elements of dense gradients that one workgroup takes without a second launch
 constexpr int COUNTERS = 16;             // of finished workgroups, 128 bytes apart, behind them the one of finished counters
 
 // What the plan knows of a tensor (device memory, written once).
@@ -503,7 +504,7 @@ struct NormArgs {
   uint8_t kind[GROUP];
   RowsOf rows[GROUP_ROWS];
   int64_t rows_cols[GROUP_ROWS], rows_of[GROUP_ROWS];
-  int32_t count, chunks, add;
+  int32_t count, chunks, chunk, add;      // chunk: elements of one
   double max_norm;
   double* part;
   float* out;                             // one workgroup is all: it writes the result itself
@@ -532,68 +533,73 @@ __device__ __forceinline__ void norm_result(double sum, double max_norm, float* 
   out[1] = !(norm < (double)INFINITY) ? __uint_as_float(0x7fc00000u) : norm > max_norm ? (float)(max_norm / norm) : 1.f;
 }
 
-// Squares of a chunk, sixteen bytes a thread at a time.
+// Squares of the elements from `base` to `end`, sixteen bytes a thread at a time, four times requested together; the last few one a thread.
 template <bool BF>
-__device__ __forceinline__ double chunk_squares(const void* g, int64_t base, int64_t n, int threads) {
+__device__ __forceinline__ double squares(const void* g, int64_t base, int64_t end, int threads) {
   constexpr int VEC = BF ? 8 : 4, AHEAD = 4;
   double sum[2] = {0.0, 0.0};
-  const int64_t end = std::min(base + NORM_CHUNK, n), step = (int64_t)threads * VEC;
-  int64_t i = base + (int64_t)threadIdx.x * VEC;
-  for (; i + (AHEAD - 1) * step + VEC <= end; i += AHEAD * step) {
+  const int64_t step = (int64_t)threads * VEC, whole = end - (end - base) % VEC;
+  for (int64_t i = base + (int64_t)threadIdx.x * VEC; i < whole; i += AHEAD * step) {
     Piece<BF, VEC> p[AHEAD];
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q) p[q].load(g, i + q * step);
+    for (int q = 0; q < AHEAD; ++q) {
+      p[q].clear();
+      if (i + q * step < whole) p[q].load(g, i + q * step);
+    }
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) sum[e & 1] = fma((double)p[q].value(e), (double)p[q].value(e), sum[e & 1]);
   }
-  for (; i < end; i += step)
-    for (int e = 0; e < VEC && i + e < end; ++e) {
-      const double x = (double)load_element<BF>(g, i + e);
-      sum[e & 1] = fma(x, x, sum[e & 1]);
-    }
+  if (whole + threadIdx.x < end) {
+    const double x = (double)load_element<BF>(g, whole + threadIdx.x);
+    sum[0] = fma(x, x, sum[0]);
+  }
   return sum[0] + sum[1];
 }
 // The same of a gradient by rows: rows that belong to no row of the tensor hold nothing.  Long rows are taken one by one, so that whether a row is there is
 // asked once; of short ones each thread asks for its own.
 template <bool BF>
-__device__ __forceinline__ double chunk_squares_of_rows(const void* g, const int32_t* owner, int64_t cols, int64_t base, int64_t n, int threads) {
+__device__ __forceinline__ double squares_of_rows(const void* g, const int32_t* owner, int64_t cols, int64_t base, int64_t end, int threads) {
   if (cols >= 1024) {
     double sum = 0.0;
-    const int64_t end = std::min(base + NORM_CHUNK, n);
     int64_t row = base / cols;
     for (int64_t at = base; at < end; ++row) {
       const int64_t to = std::min((row + 1) * cols, end);
-      if (owner[row] >= 0) sum += chunk_squares<BF>(g, at, to, threads);
+      if (owner[row] >= 0) sum += squares<BF>(g, at, to, threads);
       at = to;
     }
     return sum;
   }
+  // quads of columns, four a thread requested together; cols < 1024 here, so a chunk's rows and columns are 32-bit numbers
+  constexpr int AHEAD = 4;
   double sum = 0.0;
-  const int64_t end = std::min(base + NORM_CHUNK, n), row0 = base / cols, col0 = base - row0 * cols;
-  for (int64_t i = base + (int64_t)threadIdx.x * 4; i < end; i += (int64_t)threads * 4) {
-    const uint64_t c = (uint64_t)(col0 + (i - base));
-    int64_t row, col;
-    if (cols < (int64_t(1) << 31)) {
-      const uint32_t q = (uint32_t)c / (uint32_t)cols;
-      row = row0 + q; col = (int64_t)((uint32_t)c - q * (uint32_t)cols);
-    } else {
-      row = row0 + (int64_t)(c / (uint64_t)cols); col = (int64_t)(c % (uint64_t)cols);
+  const int64_t row0 = base / cols;
+  const uint32_t width = (uint32_t)cols, col0 = (uint32_t)(base - row0 * cols), n = (uint32_t)(end - base), step = (uint32_t)threads * 4;
+  const int32_t* const own = owner + row0;
+  for (uint32_t i = threadIdx.x * 4; i < n; i += AHEAD * step) {
+    Piece<BF, 4> p[AHEAD];
+    bool there[AHEAD];
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      const uint32_t c = col0 + i + q * step, row = c / width, col = c - row * width;
+      there[q] = i + q * step + 4 <= n && col + 4 <= width && own[row] >= 0;
     }
-    if (i + 4 <= end && col + 4 <= cols) {
-      if (owner[row] < 0) continue;
-      float x[4];
-      load_quad<BF, false>(g, i, x);
-      for (int e = 0; e < 4; ++e) sum = fma((double)x[e], (double)x[e], sum);
-    } else {
-      for (int e = 0; e < 4 && i + e < end; ++e) {
-        if (owner[row] >= 0) {
-          const double x = (double)load_element<BF>(g, i + e);
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      p[q].clear();
+      if (there[q]) p[q].load(g, base + i + q * step);
+    }
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) {
+      for (int e = 0; e < 4; ++e) sum = fma((double)p[q].value(e), (double)p[q].value(e), sum);
+      const uint32_t at = i + q * step, c = col0 + at;
+      if (there[q] || at >= n || (at + 4 <= n && c % width + 4 <= width)) continue;
+      for (uint32_t e = 0; e < 4 && at + e < n; ++e)   // over the end of a row or of the chunk: one by one
+        if (own[(c + e) / width] >= 0) {
+          const double x = (double)load_element<BF>(g, base + at + e);
           sum = fma(x, x, sum);
         }
-        if (++col == cols) { col = 0; ++row; }
-      }
     }
   }
   return sum;
@@ -607,15 +613,15 @@ __global__ __launch_bounds__(1024) void k_norm_part(NormArgs a) {
   for (int32_t c = (int32_t)blockIdx.x; c < a.chunks; c += (int32_t)gridDim.x) {
     while (k + 1 < a.count && a.first[k + 1] <= c) ++k;
     const int32_t chunks = (k + 1 < a.count ? a.first[k + 1] : a.chunks) - a.first[k];
-    const int64_t n = (int64_t)chunks * NORM_CHUNK - a.missing[k], base = (int64_t)(c - a.first[k]) * NORM_CHUNK;
+    const int64_t base = (int64_t)(c - a.first[k]) * a.chunk, end = std::min(base + a.chunk, (int64_t)chunks * a.chunk - a.missing[k]);
     const uint8_t kind = a.kind[k];
     if (kind & G_ROWS) {
       const int r = kind >> 2;
       const int32_t* owner = a.rows[r].index + a.rows_of[r];
-      sum += kind & G_BF16 ? chunk_squares_of_rows<true>(a.g[k], owner, a.rows_cols[r], base, n, threads)
-                           : chunk_squares_of_rows<false>(a.g[k], owner, a.rows_cols[r], base, n, threads);
+      sum += kind & G_BF16 ? squares_of_rows<true>(a.g[k], owner, a.rows_cols[r], base, end, threads)
+                           : squares_of_rows<false>(a.g[k], owner, a.rows_cols[r], base, end, threads);
     } else {
-      sum += kind & G_BF16 ? chunk_squares<true>(a.g[k], base, n, threads) : chunk_squares<false>(a.g[k], base, n, threads);
+      sum += kind & G_BF16 ? squares<true>(a.g[k], base, end, threads) : squares<false>(a.g[k], base, end, threads);
     }
   }
   sum = block_sum(sum, sums);
@@ -920,18 +926,28 @@ int lordo_grad_norm(const lordo_grad* G, int32_t n, double max_norm, float* out,
   if ((reinterpret_cast<uintptr_t>(out) & 3) != 0 || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return LORDO_EINVAL;
   if (workspace_bytes < LORDO_NORM_WORKSPACE_BYTES) return LORDO_ENOMEM;
   auto elements = [](const lordo_grad& g) { return g.index ? g.slots * g.cols : g.rows * g.cols; };
-  int64_t all = 0;
+  int64_t all = 0, chunk = NORM_CHUNK, chunks = 0;
+  bool by_rows = false;
   for (int i = 0; i < n; ++i) {
     if (!good_grad(G[i])) return LORDO_EINVAL;
-    all += (elements(G[i]) + NORM_CHUNK - 1) / NORM_CHUNK;
-    if (all > (int64_t(1) << 30)) return LORDO_EINVAL;
+    all += elements(G[i]);
+    by_rows |= G[i].index != nullptr;
+    chunks += (elements(G[i]) + chunk - 1) / chunk;
+    if (chunks > (int64_t(1) << 30)) return LORDO_EINVAL;
+  }
+  if (chunks < NORM_BLOCKS) {
+    chunk = NORM_SMALL_CHUNK;
+    chunks = 0;
+    for (int i = 0; i < n; ++i) chunks += (elements(G[i]) + chunk - 1) / chunk;
   }
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const int blocks = (int)std::min<int64_t>(std::max<int64_t>(all, 1), NORM_BLOCKS);      // of every launch: each adds to the sums of the one before
-  const bool one = n <= GROUP && all <= NORM_ALONE;
+  const int blocks = (int)std::min<int64_t>(std::max<int64_t>(chunks, 1), NORM_BLOCKS);      // of every launch: each adds to the sums of the one before
+  const bool one = n <= GROUP && all <= NORM_ALONE && !by_rows;
+  if (one) chunk = NORM_CHUNK;
   NormArgs a;
   a.part = reinterpret_cast<double*>(workspace);
   a.max_norm = max_norm;
+  a.chunk = (int32_t)chunk;
   a.out = nullptr;
   for (int at = 0; at < n;) {
     a.count = 0;
@@ -940,17 +956,17 @@ int lordo_grad_norm(const lordo_grad* G, int32_t n, double max_norm, float* out,
     for (int rows = 0; at + a.count < n && a.count < GROUP; ++a.count) {
       const lordo_grad& g = G[at + a.count];
       if (g.index && rows == GROUP_ROWS) break;
-      const int64_t m = elements(g), chunks = (m + NORM_CHUNK - 1) / NORM_CHUNK;
+      const int64_t m = elements(g), mine = (m + chunk - 1) / chunk;
       a.g[a.count] = g.data;
       a.first[a.count] = a.chunks;
-      a.missing[a.count] = (uint16_t)(chunks * NORM_CHUNK - m);
+      a.missing[a.count] = (uint16_t)(mine * chunk - m);
       a.kind[a.count] = grad_kind(g, rows);
       if (g.index) {
         a.rows[rows] = RowsOf{g.index, (int32_t)g.slots};
         a.rows_cols[rows] = g.cols;
         a.rows_of[rows++] = g.rows;
       }
-      a.chunks += (int32_t)chunks;
+      a.chunks += (int32_t)mine;
     }
     at += a.count;
     if (one && at == n && !a.add) {
