@@ -340,13 +340,13 @@ int lordo_profile_read(lordo_ctx* ctx, int32_t kernel_class, double* total_ms, i
 #define LORDO_Q8  2            /* moments in 8 bits, see lordo_adamw_hparams.state_dtype */
 #define LORDO_I32 3            /* types of token ids */
 #define LORDO_I64 4
-#define LORDO_MAX_TOKENS     (1 << 26)
+#define LORDO_MAX_TOKENS     (1 << 25)
 #define LORDO_MAX_VOCAB      (1 << 22)
 #define LORDO_MAX_EMBED_COLS (1 << 20)
 
 typedef struct lordo_adamw lordo_adamw;
 
-/* One tensor: at most 2^38 elements; decay 1: the weight decay applies to it, 0: it does not (norm weights, biases). */
+/* One tensor, of a set of less than 2^36 elements in all; decay 1: the weight decay applies to it, 0: it does not (norm weights, biases). */
 typedef struct {
   int64_t rows, cols;
   int32_t decay;
@@ -394,7 +394,7 @@ int lordo_adamw_init(lordo_adamw** out, const lordo_tensor* tensors, int32_t n, 
  *   t <- t+1;  g = grad_scale * clip[1] * G;  u <- beta1 u + (1-beta1) g;  v <- beta2 v + (1-beta2) g*g;
  *   W <- W - lr * ((u/c1) / (sqrt(v/c2) + eps) + weight_decay W),  c_i = 1-beta_i^t (1 if bias_correction == 0);
  *   0/0 (eps = 0, no gradient so far) is 0.
- *   W     host array of n device pointers, updated in place.
+ *   W     host array of n device pointers, updated in place; no two tensors may overlap.
  *   G     host array of n gradients of the tensors' rows and cols, read only.  Rows that a gradient by rows does not have get a gradient of
  *         zero: their moments and weights decay as in any step.
  *   clip  device, two floats as lordo_grad_norm leaves them, or NULL (coefficient 1).  With a coefficient that is not finite the whole step is

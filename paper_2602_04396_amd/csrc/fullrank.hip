@@ -262,7 +262,8 @@ struct StepScalars {
 };
 
 // u / (sqrt(v) + eps) by the approximate root and reciprocal (one unit in the last place each).  The root does not take subnormal numbers, and gives 0 or what
-// it should, at most 2^-63: nothing beside an eps from 2^-38 on.  Below that the argument is scaled, and a sum of 0 (eps = 0, no gradient so far) gives 0.
+// it should, at most 2^-63: nothing beside an eps from 2^-38 on.  Below that the argument is scaled, and a sum of 0 (eps = 0, no gradient so far), or one that the
+// reciprocal does not take, gives 0.
 __device__ __forceinline__ void updates_of(const float (&u)[4], const float (&v)[4], float eps, float (&n)[4]) {
   if (eps >= 0x1p-38f) {                               // (uniform)
 #pragma unroll
@@ -272,7 +273,7 @@ __device__ __forceinline__ void updates_of(const float (&u)[4], const float (&v)
     for (int e = 0; e < 4; ++e) {
       const bool small = v[e] < 0x1p-96f;
       const float den = fmaf(__builtin_amdgcn_sqrtf(small ? v[e] * 0x1p64f : v[e]), small ? 0x1p-32f : 1.f, eps);
-      n[e] = den == 0.f ? 0.f : u[e] * __builtin_amdgcn_rcpf(den);
+      n[e] = den < 0x1p-126f ? 0.f : u[e] * __builtin_amdgcn_rcpf(den);
     }
   }
 }
@@ -696,7 +697,7 @@ int plan_adamw(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams
     if (s.rows <= 0 || s.cols <= 0 || s.rows > (int64_t(1) << 38) || s.cols > (int64_t(1) << 38) / s.rows) return LORDO_EINVAL;
     if ((s.decay != 0 && s.decay != 1) || s.reserved != 0) return LORDO_EINVAL;
     chunks += (s.rows * s.cols + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
-    if (chunks > (int64_t(1) << 30)) return LORDO_EINVAL;
+    if (chunks >= int64_t(1) << 24) return LORDO_EINVAL;           // (a launch has less than 2^32 threads)
   }
   c.chunk = chunks >= ADAMW_MANY ? ADAMW_CHUNK : ADAMW_SMALL_CHUNK;
   chunks = 0;
@@ -900,7 +901,7 @@ int lordo_adamw_get_step(lordo_adamw* c, int64_t* t) {
 }
 
 int lordo_adamw_set_step(lordo_adamw* c, int64_t t) {
-  if (!c || t < 0) return LORDO_EINVAL;
+  if (!c || t < 0 || t > (int64_t(1) << 62)) return LORDO_EINVAL;
   c->t = t;
   c->step_dirty = true;
   return LORDO_OK;

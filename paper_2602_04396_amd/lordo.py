@@ -31,7 +31,7 @@ EXPORTS = [
 ]
 STATIC_WORKSPACE_BYTES = 64 << 20
 NORM_WORKSPACE_BYTES = 8192
-MAX_TOKENS, MAX_VOCAB = 1 << 26, 1 << 22
+MAX_TOKENS, MAX_VOCAB = 1 << 25, 1 << 22
 K_DOWN, K_ADAM, K_UP, K_OUTER, K_EXPORT, K_REFRESH = range(6)
 
 
@@ -520,6 +520,7 @@ class AdamW:
         self.ctx = C.c_void_p()
         self.shapes = [tuple(sh) for sh in shapes]
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        self.made_for = (self.device, hp.param_dtype, tuple(sh[:2] for sh in self.shapes))
         self.at = self.device.index
         if self.at != torch.cuda.current_device():
             raise ValueError(f"{self.device} is not the current device")
@@ -538,6 +539,8 @@ class AdamW:
     def ptrs(self, W) -> PtrList:
         """Validate the list of weights once and freeze its pointers for repeated calls."""
         if isinstance(W, PtrList):
+            if getattr(W, "made_for", None) != self.made_for:
+                raise ValueError("a list of weights made for other shapes")
             return W
         dtype = self.torch.bfloat16 if self.hp.param_dtype == BF16 else self.torch.float32
         if len(W) != len(self.shapes):
@@ -545,11 +548,16 @@ class AdamW:
         for t, sh in zip(W, self.shapes):
             if _rows_cols(t) != sh[:2] or t.dtype != dtype or not t.is_contiguous() or t.device != self.device:
                 raise ValueError(f"expected a contiguous {dtype} tensor of shape {sh[:2]} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return PtrList(list(W), _ptr_array(W))
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in W)
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("two of the weights overlap: a tensor is stepped once")
+        p = PtrList(list(W), _ptr_array(W))
+        p.made_for = self.made_for
+        return p
 
     def local_step(self, W, G, lr, grad_scale=1.0, clip=None):
         """One step; the gradient is grad_scale * clip[1] * G (clip: what grad_norm returned, or None)."""
-        if not isinstance(W, PtrList):
+        if getattr(W, "made_for", None) is not self.made_for:
             W = self.ptrs(W)
         if not isinstance(G, GradList):
             G = GradList(G)

@@ -37,7 +37,7 @@ def test_workspace_holds_the_moments(lib):
     assert rc == lordo.OK and 2 * padded + padded // 64 <= small <= 2 * padded + padded // 64 + 4096
 
 
-@pytest.mark.parametrize("shapes", [[(0, 4)], [(4, 0)], [(-1, 4)], [(1 << 20, (1 << 18) + 1)], [(1 << 39, 1)], [(4, 4, 2, 0)], [(4, 4, 1, 1)]])
+@pytest.mark.parametrize("shapes", [[(0, 4)], [(4, 0)], [(-1, 4)], [(1 << 20, (1 << 18) + 1)], [(1 << 39, 1)], [(1 << 18, 1 << 18)], [(1 << 17, 1 << 18), (1 << 17, 1 << 18)], [(4, 4, 2, 0)], [(4, 4, 1, 1)]])
 def test_bad_shapes(lib, shapes):
     assert _bytes(lib, shapes, lordo.adamw_hparams())[0] == lordo.EINVAL
 
@@ -137,6 +137,17 @@ def test_embedding_workspace(lib):
     assert lib.lordo_embed_workspace_bytes(8, 10, 6, None) == lordo.EINVAL
     # no tokens, nothing to do
     assert lib.lordo_embed_lookup(None, lordo.F32, 10, 6, None, lordo.I64, 0, 1.0, None, lordo.F32, None) == lordo.OK
+
+
+def test_without_a_gpu(lib):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    p, ctx = C.c_void_p(1 << 20), C.c_void_p()
+    assert lib.lordo_adamw_init(C.byref(ctx), _tensors((4, 4)), 1, C.byref(lordo.adamw_hparams()), p, 1 << 20, None) == lordo.EHIP and not ctx.value
+    assert lib.lordo_grad_norm(_grad(), 1, 1.0, 4096, p, lordo.NORM_WORKSPACE_BYTES, None) == lordo.EHIP
+    assert lib.lordo_embed_lookup(4096, lordo.F32, 10, 6, 4096, lordo.I64, 8, 1.0, 8192, lordo.F32, None) == lordo.EHIP
+    assert lib.lordo_embed_gradient(4096, lordo.I64, 8, 4096, lordo.F32, 10, 6, 1.0, -1, 0, 8192, lordo.F32, p, 1 << 20, None) == lordo.EHIP
 
 
 def test_binding_refuses_host_tensors():

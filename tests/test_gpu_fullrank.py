@@ -106,14 +106,14 @@ def test_options(torch, state):
     from paper_2602_04396_amd import lordo
     shapes, gen = [(1, 700), (5, 128)], _gen(torch, 6)
     q = lordo.Q8 if state == "q8" else lordo.F32
-    for kw, t0 in ((dict(eps=0.0), 0), (dict(bias_correction=False, weight_decay=0.3), 0), (dict(beta1=0.0, beta2=0.0), 7), (dict(), 10 ** 9)):
+    for kw, t0 in ((dict(eps=0.0), 0), (dict(eps=2.0 ** -100, beta2=1 - 2.0 ** -40), 0), (dict(eps=1e-13), 5), (dict(bias_correction=False, weight_decay=0.3), 0), (dict(beta1=0.0, beta2=0.0), 7), (dict(), 10 ** 9)):
         opt = lordo.AdamW(shapes, lordo.adamw_hparams(state_dtype=q, **kw), torch)
         opt.step = t0
         W = [_tensor(torch, gen, *sh, torch.float32, 0.02) for sh in shapes]
         for k in range(2):
             G = [_tensor(torch, gen, *sh, torch.float32, 1.0) for sh in shapes]
             G[0].mul_(torch.exp2(torch.randn(G[0].shape, generator=gen, device="cuda") * 12))
-            if "eps" in kw:
+            if kw.get("eps", 1) < 1e-20:
                 G[0][:, 100:] = 0
                 G[1].zero_()
             _check_step(torch, opt, shapes, W, G, 1e-2 if k == 0 else 0.0)
@@ -328,6 +328,15 @@ def test_refusals_of_a_context(torch):
     for bad in ([torch.zeros(8, 4, device="cuda")], [G[0], G[0]], [torch.zeros(4, 8, device="cuda", dtype=torch.float16)]):
         with pytest.raises((ValueError, lordo.LordoError)):
             opt.local_step(W, bad, 1e-3)
+    flat = torch.zeros(40, device="cuda")
+    two = lordo.AdamW([(4, 8), (1, 8)], lordo.adamw_hparams(), torch)
+    with pytest.raises(ValueError):                          # a tensor twice, or a part of it
+        two.local_step([flat[:32].view(4, 8), flat[24:32]], [G[0], G[0][0]], 1e-3)
+    both = two.ptrs([flat[:32].view(4, 8), flat[32:]])
+    with pytest.raises(ValueError):
+        opt.local_step(both, G, 1e-3)
+    with pytest.raises(lordo.LordoError):
+        opt.step = 2 ** 63 - 1
     with pytest.raises(lordo.LordoError):
         opt.local_step(W, G, float("nan"))
     with pytest.raises(lordo.LordoError):
@@ -344,3 +353,5 @@ def test_refusals_of_a_context(torch):
     for w in (null, odd):
         assert lib.lordo_adamw_step(opt.ctx, w, arr, 1e-3, 1.0, None, None) == lordo.EINVAL
     assert not W[0].any() and opt.step == 0
+    again = lordo.AdamW([(4, 8)], lordo.adamw_hparams(), torch)          # the same shapes: the list is good for both
+    again.local_step(opt.ptrs(W), G, 1e-3)
