@@ -35,6 +35,8 @@ __device__ __forceinline__ int32_t token_key(const Ids& ids, int64_t t) {
 }
 
 // A thread copies eight columns of ROWS rows, all requested before the first is written.  NARROW: rows shorter than that, a thread an element.
+// Memory: 32768 tokens, an eighth of them padding, of a 32000 x 2048 fp32 table to bf16 49 us: 134 MB written and 235 read, two thirds of that from the caches (four
+// columns of one row a thread: 58 us).
 template <bool IN_BF, bool OUT_BF, int ROWS, bool NARROW>
 __global__ __launch_bounds__(256) void k_lookup(const void* table, Ids ids, int64_t tokens, int64_t cols, int lanes_log2, float scale, void* out) {
   constexpr int VEC = NARROW ? 1 : 8;
@@ -82,6 +84,7 @@ __device__ __forceinline__ void fill_share(const Fill& f, int64_t first, int64_t
 // Order of up to 8192 tokens in one launch.  Key and position in one 32-bit number are all different, so the place of a token is how many numbers are
 // smaller: all pairs are compared, two instructions a pair, with the other side read from LDS, four numbers a (broadcast) read.  A workgroup places 32 tokens: the two
 // halves of a wave compare them with different numbers, its sixteen waves with a 32nd of the batch each half.  8192 tokens are 256 workgroups, one a compute unit.
+// 4095 tokens 5.7 us, 8192 9.8, of which 3 are comparisons; the two digits that 64k tokens need take 27 without what they fill, so comparing ends at 8192.
 __global__ __launch_bounds__(1024) void k_rank(Ids ids, int32_t tokens, int pos_bits, Sorted out, int rank_blocks, Fill fill) {
   if ((int)blockIdx.x >= rank_blocks) {
     fill_share(fill, (int64_t)((int)blockIdx.x - rank_blocks) * 1024 + threadIdx.x, (int64_t)((int)gridDim.x - rank_blocks) * 1024);
@@ -118,6 +121,8 @@ __global__ __launch_bounds__(1024) void k_rank(Ids ids, int32_t tokens, int pos_
 
 // More tokens: by the digits of the key, the lowest first, stable.  A workgroup has `block` consecutive tokens; k_count leaves how many of each digit it
 // holds, k_place adds up what is before it (smaller digits anywhere, its own in earlier workgroups) and moves its tokens there.
+// Latency: 65536 tokens with ids of 15 bits 5 + 8 us a digit (comparing all pairs: 639 us), or 13 to 15 a launch with a quarter of 262 MB of zeros each, which hide
+// it (all zeros in the first launch: 52 + 12 + 5 + 11).
 struct Digit { int32_t tokens, block, blocks, shift, bits; };
 
 template <bool FIRST>
@@ -242,6 +247,8 @@ struct GradOut {
 // end, so a tile works on at most two tiles of tokens and only longer runs leave partial rows: one of the tile they begin in (slot 1), one
 // of each tile they go on in (slot 0).  Every wave holds ids and positions of both tiles, a lane one; rows are requested eight at a time, with
 // them what the output holds where the sums are added to it.  NARROW: rows shorter than a piece, a thread an element.
+// HBM: 57344 of 65536 rows of 2048 bf16 summed to 13000 of fp32: 63 us, 5.5 TB/s (one row in flight: 142 us); 8192 rows of 4096 fp32 to 3500: 32 us.
+// 4095 rows of 1023 bf16 added: 7.8 us, latency (what the output holds requested at the end of each run: 47 us).
 template <bool IN_BF, bool OUT_BF, bool ADD, bool NARROW>
 __global__ __launch_bounds__(256) void k_tile_sum(const void* dy, Sorted in, int32_t tokens, int32_t tile_tokens, int32_t vocab, int64_t cols, GradOut o) {
   constexpr int VEC = NARROW ? 1 : IN_BF ? 8 : 4, AHEAD = 8;
@@ -314,6 +321,7 @@ __global__ __launch_bounds__(256) void k_tile_sum(const void* dy, Sorted in, int
 
 // Runs longer than two tiles: the partial rows of each in order.  A workgroup looks at one tile, 1024 columns of it; its four groups of four waves take consecutive
 // shares of the tiles that a run goes on in.
+// Latency of three dependent loads and the launch: 6 to 10 us (65536 tokens; 46 with sixteen tiles a workgroup and one request in flight).
 template <bool OUT_BF>
 __global__ __launch_bounds__(1024) void k_join_tiles(Sorted in, int32_t tokens, int32_t tile_tokens, int32_t vocab, int64_t cols, GradOut o) {
   const int32_t tile = (int32_t)blockIdx.x, first = tile * tile_tokens, tiles = (tokens + tile_tokens - 1) / tile_tokens;
