@@ -482,7 +482,7 @@ int embed_gradient(Ids ids, int64_t tokens, const void* dy, int32_t dy_dtype, in
     const int digits = (key_bits + 8) / 9;
     d.bits = (key_bits + digits - 1) / digits;
     // every launch fills a share, while its own few workgroups wait for memory
-    const int64_t share = (fill.bytes / (2 * digits) + 65535) / 65536 * 65536;
+    const int64_t piece = 65536 * 2 * digits, share = (fill.bytes + piece - 1) / piece * 65536;
     auto next_fill = [&] {
       Fill f = fill;
       f.bytes = std::min(share, fill.bytes);

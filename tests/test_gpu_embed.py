@@ -138,6 +138,28 @@ def test_gradient_of_many_tokens(torch, tokens, vocab, cols, kind):
     assert torch.equal(by_rows.rows[slot[slot >= 0]], out[slot >= 0])
 
 
+def test_outputs_just_above_whole_shares_are_filled_to_their_end(torch):
+    """More than 8192 tokens: 64 KB pieces of the fill are spread over two launches a digit.  262146 bytes are four such pieces and one bf16 element
+    (ids of 16 bits, two digits), 1572868 bytes are 24 and one int32 (ids of 19 bits, three digits): the last element is written too."""
+    from paper_2602_04396_amd import lordo
+    tokens, vocab, cols = 8193, 43691, 3
+    assert vocab * cols * 2 == 4 * 65536 + 2
+    ids = torch.arange(tokens, device="cuda")
+    dy = torch.ones(tokens, cols, device="cuda")
+    out = lordo.embed_gradient(ids, dy, torch.full((vocab, cols), 9.0, device="cuda", dtype=torch.bfloat16))
+    assert torch.all(out[:tokens] == 1.0) and torch.all(out[tokens:] == 0.0)
+    tokens, vocab = 93217, 300000
+    assert 4 * (vocab + tokens) == 24 * 65536 + 4
+    ids = torch.arange(tokens, device="cuda") // 2
+    dy = torch.ones(tokens, 1, device="cuda")
+    ids[-1] = ids[-2]                                    # (the last slot holds no row)
+    got = lordo.RowGrad(torch.full((tokens, 1), 7.0, device="cuda"), torch.full((vocab + tokens,), 5, device="cuda", dtype=torch.int32), vocab)
+    lordo.embed_gradient_rows(ids, dy, vocab, out=got)
+    owner = got.index[vocab:]
+    assert int((owner >= 0).sum()) == int(ids[-1]) + 1 and int(owner[-1]) == -1
+    assert int((got.index[:vocab] >= 0).sum()) == int(ids[-1]) + 1
+
+
 def test_refusals(torch):
     from paper_2602_04396_amd import lordo
     table, ids, dy = torch.zeros(8, 4, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda"), torch.zeros(3, 4, device="cuda")
