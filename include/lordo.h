@@ -335,7 +335,8 @@ int lordo_profile_read(lordo_ctx* ctx, int32_t kernel_class, double* total_ms, i
  *   - a tensor is rows x cols, row-major and contiguous (a vector: 1 x cols), from any element on;
  *   - the calls without a context work on the GPU that is current, where all their arrays have to live;
  *   - a workspace is scratch between the start and the end of one call: calls that may run at the same time (two streams,
- *     two recorded graphs) need one each.
+ *     two recorded graphs) need one each;
+ *   - scale, grad_scale, lr and lr * weight_decay have to be finite as fp32 numbers.
  * ------------------------------------------------------------------------------------------------------------- */
 #define LORDO_Q8  2            /* moments in 8 bits, see lordo_adamw_hparams.state_dtype */
 #define LORDO_I32 3            /* types of token ids */
@@ -408,7 +409,8 @@ int lordo_adamw_step(lordo_adamw* ctx, void* const* W, const lordo_grad* G, doub
  *   lordo_adamw_sync_payload    *dev_ptr: the array itself, in the arena (averaged in place as with lordo_sync_payload); NULL with LORDO_Q8.
  *                               *count: its elements
  *   lordo_adamw_export_moments  dst[count] <- the moments (8-bit ones: the values they stand for, rounded to fp32)
- *   lordo_adamw_import_moments  the moments <- src[count]; 8-bit ones with theta = 1/2 (what was exported comes back as it was) and |v| */
+ *   lordo_adamw_import_moments  the moments <- src[count]; 8-bit ones with theta = 1/2 and |v|: what was exported comes back as
+ *                               it was, but for values below 2^-146, which fp32 holds with fewer bits or as 0 */
 int lordo_adamw_sync_payload(lordo_adamw* ctx, void** dev_ptr, size_t* count);
 int lordo_adamw_export_moments(lordo_adamw* ctx, float* dst, void* stream);
 int lordo_adamw_import_moments(lordo_adamw* ctx, const float* src, void* stream);

@@ -530,7 +530,7 @@ extern "C" {
 
 int lordo_embed_lookup(const void* table, int32_t table_dtype, int64_t vocab, int64_t cols, const void* ids, int32_t ids_dtype, int64_t tokens,
                        double scale, void* out, int32_t out_dtype, void* stream) {
-  if (!good_table(vocab, cols) || !good_ids(ids, ids_dtype, tokens) || !float_type(table_dtype) || !float_type(out_dtype) || !std::isfinite(scale))
+  if (!good_table(vocab, cols) || !good_ids(ids, ids_dtype, tokens) || !float_type(table_dtype) || !float_type(out_dtype) || !finite_in_fp32(scale))
     return LORDO_EINVAL;
   if (tokens == 0) return LORDO_OK;
   if (!table || !out || !float_aligned(table, table_dtype) || !float_aligned(out, out_dtype)) return LORDO_EINVAL;
@@ -547,7 +547,7 @@ int lordo_embed_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols, siz
 
 int lordo_embed_gradient(const void* ids, int32_t ids_dtype, int64_t tokens, const void* dy, int32_t dy_dtype, int64_t vocab, int64_t cols, double scale,
                          int64_t pad_id, int32_t accumulate, void* dw, int32_t dw_dtype, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!good_table(vocab, cols) || !good_ids(ids, ids_dtype, tokens) || !float_type(dy_dtype) || !float_type(dw_dtype) || !std::isfinite(scale))
+  if (!good_table(vocab, cols) || !good_ids(ids, ids_dtype, tokens) || !float_type(dy_dtype) || !float_type(dw_dtype) || !finite_in_fp32(scale))
     return LORDO_EINVAL;
   if ((accumulate != 0 && accumulate != 1) || !dw || !float_aligned(dw, dw_dtype)) return LORDO_EINVAL;
   if (tokens > 0 && (!dy || !float_aligned(dy, dy_dtype) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0)) return LORDO_EINVAL;
@@ -558,7 +558,7 @@ int lordo_embed_gradient(const void* ids, int32_t ids_dtype, int64_t tokens, con
 
 int lordo_embed_gradient_rows(const void* ids, int32_t ids_dtype, int64_t tokens, const void* dy, int32_t dy_dtype, int64_t vocab, int64_t cols, double scale,
                               int64_t pad_id, void* rows, int32_t rows_dtype, int32_t* index, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!good_table(vocab, cols) || !good_ids(ids, ids_dtype, tokens) || !float_type(dy_dtype) || !float_type(rows_dtype) || !std::isfinite(scale))
+  if (!good_table(vocab, cols) || !good_ids(ids, ids_dtype, tokens) || !float_type(dy_dtype) || !float_type(rows_dtype) || !finite_in_fp32(scale))
     return LORDO_EINVAL;
   if (!index || (reinterpret_cast<uintptr_t>(index) & 3) != 0) return LORDO_EINVAL;
   if (tokens > 0 && (!rows || !float_aligned(rows, rows_dtype) || !dy || !float_aligned(dy, dy_dtype) || !workspace ||

@@ -4,6 +4,7 @@
 #include "../../include/lordo.h"
 #include "common.h"
 
+#include <cmath>
 #include <cstdio>
 #include <new>
 
@@ -138,6 +139,9 @@ __device__ __forceinline__ int find_tensor(const int32_t* first, int count, int3
   for (int q = 0; q < 4; ++q) k += __popcll(__ballot(64 * q + lane < count && x[q] <= c));
   return __builtin_amdgcn_readfirstlane(k - 1);
 }
+
+// A factor that reaches the kernels in fp32: neither infinite there nor NaN.
+inline bool finite_in_fp32(double x) { return std::isfinite((float)x); }
 
 // Nothing may leave a C entry point but a code.
 template <class F>

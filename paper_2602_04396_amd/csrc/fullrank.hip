@@ -1,7 +1,7 @@
 // The optimizer of what is not projected (embedding, head, norm weights, biases): AdamW over many tensors at once with moments in fp32
 // or in 8 bits, and the global gradient norm with its clip coefficient.
 //
-//   k_adamw<WBF, Q8>   t <- t + 1; u <- b1 u + (1 - b1) s g; v <- b2 v + (1 - b2)(s g)^2; W <- W - lr ((u / c1) / (sqrt(v / c2) + eps) + wd W)
+//   k_adamw<WBF, Q8, CHUNK>   t <- t + 1; u <- b1 u + (1 - b1) s g; v <- b2 v + (1 - b2)(s g)^2; W <- W - lr ((u / c1) / (sqrt(v / c2) + eps) + wd W)
 //                      and, by its last workgroup, step count and bias corrections of the next step
 //   k_moments          8-bit moments <-> the fp32 array [u | v]
 //   k_norm_part, k_norm_sum   sqrt(sum g^2) and min(1, max / norm)
@@ -16,7 +16,7 @@ namespace lordo {
 
 // Elements of one tensor that a workgroup takes: 4096, or 1024 where those would be less than 1024 workgroups (four a compute unit).
 constexpr int64_t ADAMW_CHUNK = 4096, ADAMW_SMALL_CHUNK = 1024, ADAMW_MANY = 1024;
-constexpr int Q8_BLOCK = 128;            // elements that share a scale
+constexpr int Q8_BLOCK = 128;            // elements that share an exponent
 constexpr int GROUP = 200;               // tensors of one launch, and gradients by rows among them: their pointers travel in the kernel arguments (below 4 KiB)
 constexpr int GROUP_ROWS = 8;
 // Elements of a workgroup of the norm at a time: 16384, or 2048 where those would be less than one for each of its 1024 workgroups.
@@ -435,9 +435,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   if (threadIdx.x == 0 && last_workgroup(a.flag + 32)) adamw_step_write(a.step, steps + 1, a.b1d, a.b2d, a.bias_correction);
 }
 
-// HBM: 2 x 32000 x 4096 out of 8 bits 471 us, 5.6 TB/s (2 bytes read, 8 written an element).
 // TO_STATE: moments <- [u | v], in 8 bits with thresholds of one half (a value of the grid stays itself); else [u | v] <- moments.  What lies
-// between the tensors is written as zero.
+// between the tensors is written as zero.  HBM: 2 x 32000 x 4096 out of 8 bits 471 us, 5.6 TB/s (2 bytes read, 8 written an element).
 template <bool Q8, bool TO_STATE>
 __global__ __launch_bounds__(256) void k_moments(AdamwState st, const AdamwTensor* tensors, const int32_t* first, int32_t count, int32_t chunk_elements, float* plain,
                                                  int64_t total) {
@@ -832,7 +831,7 @@ int lordo_adamw_init(lordo_adamw** out, const lordo_tensor* tensors, int32_t n, 
 }
 
 int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double lr, double grad_scale, const float* clip, void* stream) {
-  if (!c || !W || !G || !std::isfinite(lr) || !std::isfinite(grad_scale)) return LORDO_EINVAL;
+  if (!c || !W || !G || !finite_in_fp32(lr) || !finite_in_fp32(lr * c->hp.weight_decay) || !finite_in_fp32(grad_scale)) return LORDO_EINVAL;
   if (!c->on_its_device()) return LORDO_ESTATE;
   const int n = (int)c->shapes.size();
   const uintptr_t w_mask = c->hp.param_dtype == LORDO_BF16 ? 1 : 3;

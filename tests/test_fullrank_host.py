@@ -126,6 +126,15 @@ def test_bad_embedding_gradients(lib, rows, bad):
     assert rc == lordo.EINVAL
 
 
+@pytest.mark.parametrize("scale", [1e39, -1e39, 3.5e38])
+def test_a_scale_beyond_fp32(lib, scale):
+    """Infinite in fp32, where it would make the zero rows of padding NaN."""
+    ws = C.c_void_p(1 << 20)
+    assert lib.lordo_embed_lookup(4096, lordo.F32, 10, 6, 4096, lordo.I64, 8, scale, 8192, lordo.F32, None) == lordo.EINVAL
+    assert lib.lordo_embed_gradient(4096, lordo.I64, 8, 4096, lordo.F32, 10, 6, scale, -1, 0, 8192, lordo.F32, ws, 1 << 20, None) == lordo.EINVAL
+    assert lib.lordo_embed_gradient_rows(4096, lordo.I64, 8, 4096, lordo.F32, 10, 6, scale, -1, 8192, lordo.F32, 4096, ws, 1 << 20, None) == lordo.EINVAL
+
+
 def test_embedding_workspace(lib):
     size = C.c_size_t(0)
     assert lib.lordo_embed_workspace_bytes(8, 10, 6, C.byref(size)) == lordo.OK and size.value > 0

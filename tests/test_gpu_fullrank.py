@@ -316,6 +316,16 @@ def test_on_another_stream_and_recorded(torch):
         graph.reset()
 
 
+def test_factors_beyond_fp32_are_refused(torch):
+    from paper_2602_04396_amd import lordo
+    opt = lordo.AdamW([(4, 8)], lordo.adamw_hparams(weight_decay=1e3), torch)
+    W, G = [torch.ones(4, 8, device="cuda")], [torch.ones(4, 8, device="cuda")]
+    for lr, scale in ((1e39, 1.0), (1e-3, -1e39), (1e36, 1.0)):      # the last: lr times the decay
+        with pytest.raises(lordo.LordoError):
+            opt.local_step(W, G, lr, grad_scale=scale)
+    assert torch.all(W[0] == 1.0) and opt.step == 0
+
+
 def test_refusals_of_a_context(torch):
     from paper_2602_04396_amd import lordo
     lib = lordo.load()
