@@ -1,7 +1,7 @@
 // The optimizer of what is not projected (embedding, head, norm weights, biases): AdamW over many tensors at once with moments in fp32
 // or in 8 bits, and the global gradient norm with its clip coefficient.
 //
-//   k_adamw<WBF, Q8, CHUNK>   t <- t + 1; u <- b1 u + (1 - b1) s g; v <- b2 v + (1 - b2)(s g)^2; W <- W - lr ((u / c1) / (sqrt(v / c2) + eps) + wd W)
+//   k_adamw            t <- t + 1; u <- b1 u + (1 - b1) s g; v <- b2 v + (1 - b2)(s g)^2; W <- W - lr ((u / c1) / (sqrt(v / c2) + eps) + wd W)
 //                      and, by its last workgroup, step count and bias corrections of the next step
 //   k_moments          8-bit moments <-> the fp32 array [u | v]
 //   k_norm_part, k_norm_sum   sqrt(sum g^2) and min(1, max / norm)
