@@ -90,3 +90,28 @@ def embed_bound(total, size, count, out_bf16, old=None):
         total = total + old
         b = b + EPS32 * np.abs(total)
     return b * (1 + EPS16) + EPS16 * np.abs(total) if out_bf16 else b
+
+
+def in_8_bits_of_many(x, w, signed):
+    """in_8_bits for millions of elements: all blocks at once."""
+    x = np.asarray(x, dtype=np.float64)
+    pad = -x.size % BLOCK
+    b = np.pad(x, (0, pad)).reshape(-1, BLOCK)
+    theta = np.pad(np.asarray(w, dtype=np.float64), (0, pad)).reshape(-1, BLOCK) / 2 ** 17
+    lo = -126 if signed else -254
+    least = 2.0 ** math.floor(lo / 8) * (1 + (lo % 8) / 8)
+    most = np.abs(b).max(axis=1, keepdims=True).astype(np.float32).astype(np.float64)
+    held = (most > 0) & (most <= 2.0 ** 127)
+    m, e = np.frexp(np.where(held, most, 1.0))
+    scale = np.ldexp(1.0, np.maximum(np.where(m == 0.5, e - 1, e), -126))
+    y = np.minimum(np.abs(b) / scale, 1.0)
+    m, e = np.frexp(y)
+    eighths = (2 * m - 1) * 8
+    f = np.floor(eighths)
+    f = f + (eighths - f + theta >= 1)
+    q = np.minimum(np.ldexp(1 + f / 8, e - 1), 1.0)
+    under = np.where(y / least + theta >= 1, least, 0.0) if signed else np.full_like(y, least)
+    q = np.where(y < least, under, q)
+    out = np.where(y > 0, q, 0.0) * scale * np.sign(b)
+    out = np.where(held, out, np.where(most == 0, 0.0, np.nan))
+    return out.reshape(-1)[:x.size]
