@@ -369,9 +369,10 @@ typedef struct {
 
 typedef struct {
   double  beta1, beta2, eps;     /* as in lordo_hparams: in [0, 1), eps outside the root, 0 or from 2^-100 on */
-  double  weight_decay;          /* decoupled: W <- W - lr * weight_decay * W, >= 0 */
+  double  weight_decay;          /* decoupled: W <- W - lr * weight_decay * W, 0 to 2^64 */
   int32_t bias_correction;       /* as in lordo_hparams */
-  int32_t param_dtype;           /* LORDO_F32 or LORDO_BF16 storage of every W (formed in fp32, rounded to nearest-even once) */
+  int32_t param_dtype;           /* LORDO_F32 or LORDO_BF16 storage of every W (formed in fp32 with one rounding at its size, bf16 then rounded to
+                                    nearest-even once) */
   int32_t state_dtype;           /* LORDO_F32, or LORDO_Q8: both moments in 8 bits.  128 consecutive elements of a tensor share an exponent E per
                                     moment, 2^E the least power of two that their largest magnitude (in fp32) does not exceed; a value over 2^E is held as
                                     val(a) = 2^floor(a/8) (1 + (a mod 8)/8), a = 0, -1, ... : u with a sign and a >= -126, v with a >= -254, or as 0.

@@ -32,10 +32,10 @@ struct AdamwTensor {
   int32_t decay, pad_;
 };
 // Step count and what the next step takes from its bias corrections c_i = 1 - beta_i^(t + 1), kept on the device, so that a recorded step counts its replays:
-//   (u / c1) / (sqrt(v / c2) + eps) = ratio u / (sqrt(v) + eps root),   ratio = sqrt(c2) / c1, root = sqrt(c2).
+//   (u / c1) / (sqrt(v / c2) + eps) = ratio u / (sqrt(v) + eps root),   ratio = sqrt(c2) / c1, root = sqrt(c2), inverse = 1 / ratio.
 struct AdamwStep {
   int64_t t;
-  float ratio, root;
+  float ratio, root, inverse, pad_;
 };
 __device__ inline void adamw_step_write(AdamwStep* s, int64_t t, double beta1, double beta2, int bias_correction) {
   double c1 = 1.0, c2 = 1.0;
@@ -46,6 +46,7 @@ __device__ inline void adamw_step_write(AdamwStep* s, int64_t t, double beta1, d
   s->t = t;
   s->ratio = (float)(sqrt(c2) / c1);
   s->root = (float)sqrt(c2);
+  s->inverse = (float)(c1 / sqrt(c2));
 }
 __global__ void k_adamw_set(AdamwStep* s, double beta1, double beta2, int bias_correction, int64_t t) {
   adamw_step_write(s, t, beta1, beta2, bias_correction);
@@ -72,7 +73,7 @@ struct AdamwArgs {
   uint8_t kind[GROUP];
   RowsOf rows[GROUP_ROWS];
   int32_t count, advance, bias_correction; // advance: the last launch of the step moves its count on
-  float b1, omb1, b2, omb2, eps, lr, lr_wd;
+  float b1, omb1, b2, omb2, eps, lr, wd;
   double b1d, omb1d, b2d, omb2d, scale;
   const float* coef;                      // clip coefficient on the device (null: 1)
   AdamwStep* step;
@@ -256,7 +257,7 @@ __device__ __forceinline__ void load_step(Quad<Q8>& q, const Chunk& c, uint32_t 
 }
 
 struct StepScalars {
-  float scale, lr, lr_wd, eps;         // lr ratio, lr wd and eps root (AdamwStep)
+  float scale, lr, wd, eps;            // lr ratio, wd / ratio and eps root (AdamwStep)
   double omb1_scale, omb2_scale2;      // (1 - beta1) s and (1 - beta2) s^2
   uint32_t turn;
 };
@@ -324,8 +325,9 @@ __device__ __forceinline__ void store_step(Quad<Q8>& q, const AdamwArgs& a, cons
   }
   float n[4];
   updates_of(u, v, s.eps, n);
+  // the decay joins the update, so that the weight is rounded once: W - lr ratio (n + (wd / ratio) W)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) q.x[e] = fmaf(-s.lr, n[e], fmaf(-s.lr_wd, q.x[e], q.x[e]));
+  for (int e = 0; e < 4; ++e) q.x[e] = fmaf(-s.lr, fmaf(s.wd, q.x[e], n[e]), q.x[e]);
   if (cnt == 4) store_quad<WBF, true>(c.w, i, q.x);
   else
 #pragma unroll
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   s.omb1_scale = a.omb1d * scale;
   s.omb2_scale2 = a.omb2d * (scale * scale);
   s.lr = a.lr * a.step->ratio;
-  s.lr_wd = t.decay ? a.lr_wd : 0.f;
+  s.wd = t.decay ? a.wd * a.step->inverse : 0.f;
   s.eps = a.eps * a.step->root;
   const int64_t steps = a.step->t;
   s.turn = (uint32_t)(steps + 1) * Q8_STEP;
@@ -693,7 +695,7 @@ bool unit(double b) { return b >= 0 && b < 1; }
 
 int plan_adamw(const lordo_tensor* tensors, int32_t n, const lordo_adamw_hparams* hp, lordo_adamw& c) {
   if (!tensors || !hp || n <= 0) return LORDO_EINVAL;
-  if (!unit(hp->beta1) || !unit(hp->beta2) || !(hp->eps >= 0) || !std::isfinite(hp->eps) || !(hp->weight_decay >= 0) || !std::isfinite(hp->weight_decay))
+  if (!unit(hp->beta1) || !unit(hp->beta2) || !(hp->eps >= 0) || !std::isfinite(hp->eps) || !(hp->weight_decay >= 0) || !(hp->weight_decay <= 0x1p64))
     return LORDO_EINVAL;
   if (hp->eps > 0 && hp->eps < 0x1p-100) return LORDO_EINVAL;           // (see updates_of)
   if (hp->bias_correction != 0 && hp->bias_correction != 1) return LORDO_EINVAL;
@@ -850,7 +852,7 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
   a.b1 = (float)c->hp.beta1; a.omb1 = (float)(1.0 - c->hp.beta1);
   a.b2 = (float)c->hp.beta2; a.omb2 = (float)(1.0 - c->hp.beta2);
   a.b1d = c->hp.beta1; a.omb1d = 1.0 - c->hp.beta1; a.b2d = c->hp.beta2; a.omb2d = 1.0 - c->hp.beta2;
-  a.eps = (float)c->hp.eps; a.lr = (float)lr; a.lr_wd = (float)(lr * c->hp.weight_decay);
+  a.eps = (float)c->hp.eps; a.lr = (float)lr; a.wd = (float)c->hp.weight_decay;
   a.scale = grad_scale;
   a.coef = coef;
   a.step = c->step_dev();
