@@ -427,7 +427,7 @@ int lordo_adamw_poll_status(lordo_adamw* ctx, void* stream);
 void lordo_adamw_destroy(lordo_adamw* ctx);
 
 /* Global norm over n gradients and the coefficient that clips by it (Alg. 1 clip), on the device:
- *   out[0] = sqrt(sum of squares), formed in double;  out[1] = min(1, max_norm / norm), NaN if the norm is not finite.
+ *   out[0] = sqrt(sum of squares), formed in double;  out[1] = min(1, max_norm / norm), NaN if out[0] is not finite.
  *   G          gradients of any tensors (those of lordo_local_step too, whose grad_scale is out[1] read back)
  *   max_norm   > 0; infinity: no clipping
  *   workspace  device, LORDO_NORM_WORKSPACE_BYTES, 256-byte aligned

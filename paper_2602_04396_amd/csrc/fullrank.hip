@@ -539,8 +539,9 @@ __device__ __forceinline__ double block_sum(double x, double* sums) {
 }
 __device__ __forceinline__ void norm_result(double sum, double max_norm, float* out) {
   const double norm = sqrt(sum);
-  out[0] = (float)norm;
-  out[1] = !(norm < (double)INFINITY) ? __uint_as_float(0x7fc00000u) : norm > max_norm ? (float)(max_norm / norm) : 1.f;
+  const float held = (float)norm;                      // (a norm above what fp32 holds is infinite: what the caller sees decides)
+  out[0] = held;
+  out[1] = !(held < INFINITY) ? __uint_as_float(0x7fc00000u) : norm > max_norm ? (float)(max_norm / norm) : 1.f;
 }
 
 // Squares of the elements from `base` to `end`, sixteen bytes a thread at a time, four times requested together; the last few one a thread.

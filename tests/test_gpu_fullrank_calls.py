@@ -33,3 +33,24 @@ def test_the_new_weight_is_rounded_once(torch, state, rows):
     w, _, _, size = ref.adamw(w0, zero, zero, g, 1, lr, hp.beta1, hp.beta2, hp.eps, wd)
     got = W[0].double().cpu().numpy().reshape(-1)
     assert np.all(np.abs(got - w) <= ref.EPS32 * (np.abs(w) + lr * (22 * size + 8 * wd * np.abs(w0))))
+
+
+@pytest.mark.parametrize("pieces", [1, 300])
+def test_a_norm_beyond_fp32_is_not_finite(torch, pieces):
+    """Its coefficient is NaN, whatever the limit, and AdamW leaves the step out; the largest norm that fp32 holds is a norm.  In one launch and in two."""
+    from paper_2602_04396_amd import lordo
+    most = torch.finfo(torch.float32).max
+    rest = [torch.zeros(1, 3, device="cuda") for _ in range(pieces - 1)]
+    for limit in (1.0, 1e39, float("inf")):
+        out = lordo.grad_norm(rest + [torch.full((1, 4), 3e38, device="cuda")], limit)
+        assert out.tolist()[0] == float("inf") and torch.isnan(out[1])
+        out = lordo.grad_norm(rest + [torch.tensor([[0.0, -most, 1.0]], device="cuda")], limit)
+        want = np.float32(min(1.0, limit / most))
+        assert out.tolist() == [most, float(want)]
+    opt = lordo.AdamW([(1, 4)], lordo.adamw_hparams(), torch)
+    W, G = [torch.ones(1, 4, device="cuda")], [torch.full((1, 4), 3e38, device="cuda")]
+    opt.local_step(W, G, 1e-2, clip=lordo.grad_norm(rest + G))
+    assert torch.all(W[0] == 1.0) and not opt.export_moments().any()
+    with pytest.raises(lordo.LordoError) as e:
+        opt.poll_status()
+    assert e.value.code == lordo.ENUMERIC
