@@ -393,13 +393,12 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   const int32_t chunk = a.first[0] + (int32_t)blockIdx.x;
   const int k = find_tensor(a.first, a.count, chunk);
   const AdamwTensor t = a.tensors[k];
-  const float coef = a.coef ? *a.coef : 1.f;
-  if (!(fabsf(coef) < INFINITY)) {                     // the norm was not finite: this step is left out
+  const double scale = a.scale * (double)(a.coef ? *a.coef : 1.f);
+  if (!(fabsf((float)scale) < INFINITY)) {             // the norm was not finite, or the two factors together are not: this step is left out
     if (a.advance && blockIdx.x == 0 && threadIdx.x == 0) *a.flag = 1;
     return;
   }
   StepScalars s;
-  const double scale = a.scale * (double)coef;
   s.scale = (float)scale;
   s.omb1_scale = a.omb1d * scale;
   s.omb2_scale2 = a.omb2d * (scale * scale);

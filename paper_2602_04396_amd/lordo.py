@@ -611,7 +611,7 @@ class AdamW:
         _check(self.lib.lordo_adamw_set_step(self.ctx, int(t)))
 
     def poll_status(self):
-        """Raises (ENUMERIC) if a step was left out since the last poll because the clip coefficient was not finite."""
+        """Raises (ENUMERIC) if a step was left out since the last poll because the clip coefficient, or grad_scale times it, was not finite."""
         _check(self.lib.lordo_adamw_poll_status(self.ctx, self._stream()))
 
     def close(self):

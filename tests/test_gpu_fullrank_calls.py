@@ -54,3 +54,20 @@ def test_a_norm_beyond_fp32_is_not_finite(torch, pieces):
     with pytest.raises(lordo.LordoError) as e:
         opt.poll_status()
     assert e.value.code == lordo.ENUMERIC
+
+
+@pytest.mark.parametrize("state", ["f32", "q8"])
+@pytest.mark.parametrize("scale, coefficient", [(1e30, 1e30), (-1e30, 1e9), (0.0, float("inf"))])
+def test_factors_that_overflow_together_leave_the_step_out(torch, state, scale, coefficient):
+    """Each of them is finite, their product is not in fp32, where it made NaN of a gradient of zero."""
+    from paper_2602_04396_amd import lordo
+    opt = lordo.AdamW([(3, 130)], lordo.adamw_hparams(weight_decay=0.1, state_dtype=lordo.Q8 if state == "q8" else lordo.F32), torch)
+    W, G = [torch.ones(3, 130, device="cuda")], [torch.zeros(3, 130, device="cuda")]
+    opt.local_step(W, G, 1e-2, grad_scale=scale, clip=torch.tensor([1.0, coefficient], device="cuda"))
+    assert torch.all(W[0] == 1.0) and not opt.export_moments().any()
+    with pytest.raises(lordo.LordoError) as e:
+        opt.poll_status()
+    assert e.value.code == lordo.ENUMERIC
+    opt.local_step(W, G, 1e-2, grad_scale=scale / 1e30, clip=torch.tensor([1.0, 1.0], device="cuda"))
+    opt.poll_status()
+    assert torch.all(W[0] < 1.0) and not opt.export_moments().any()
