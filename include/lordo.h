@@ -417,9 +417,12 @@ int lordo_adamw_sync_payload(lordo_adamw* ctx, void** dev_ptr, size_t* count);
 int lordo_adamw_export_moments(lordo_adamw* ctx, float* dst, void* stream);
 int lordo_adamw_import_moments(lordo_adamw* ctx, const float* src, void* stream);
 
-/* Steps issued, as lordo_get_step / lordo_set_step. */
+/* Steps issued, as lordo_get_step / lordo_set_step; and the steps taken, which bias corrections and the rounding of 8-bit moments go by: replays of
+ * recorded steps counted, steps left out not.  Together with the moments and the weights they are what a run goes on from
+ * (lordo_adamw_import_moments, lordo_adamw_set_step).  lordo_adamw_steps_taken synchronises `stream`. */
 int lordo_adamw_get_step(lordo_adamw* ctx, int64_t* t);
 int lordo_adamw_set_step(lordo_adamw* ctx, int64_t t);
+int lordo_adamw_steps_taken(lordo_adamw* ctx, int64_t* t, void* stream);
 
 /* Synchronise `stream` and return LORDO_ENUMERIC if a step was left out since the last poll (cleared), else LORDO_OK. */
 int lordo_adamw_poll_status(lordo_adamw* ctx, void* stream);

@@ -845,8 +845,8 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (c->step_dirty) {
     ADAMW_CHK(launch_adamw_set(c->step_dev(), c->hp.beta1, c->hp.beta2, c->hp.bias_correction, c->t, s), "k_adamw_set");
+    c->step_dirty = false;      // (a call that fails below leaves the device count right: the last launch alone moves it on)
   }
-  c->step_dirty = true;         // until the whole step is enqueued: a call that fails below leaves the device count to be set back from `t`
   const float* const coef = clip ? clip + 1 : nullptr;
   AdamwArgs a;
   a.b1 = (float)c->hp.beta1; a.omb1 = (float)(1.0 - c->hp.beta1);
@@ -882,7 +882,6 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
     if (rc != LORDO_OK) return rc;
   }
   ++c->t;
-  c->step_dirty = false;
   return LORDO_OK;
 }
 
@@ -908,6 +907,16 @@ int lordo_adamw_import_moments(lordo_adamw* c, const float* src, void* stream) {
 int lordo_adamw_get_step(lordo_adamw* c, int64_t* t) {
   if (!c || !t) return LORDO_EINVAL;
   *t = c->t;
+  return LORDO_OK;
+}
+
+int lordo_adamw_steps_taken(lordo_adamw* c, int64_t* t, void* stream) {
+  if (!c || !t) return LORDO_EINVAL;
+  if (!c->on_its_device()) return LORDO_ESTATE;
+  ADAMW_CHK(hipStreamSynchronize(reinterpret_cast<hipStream_t>(stream)), "hipStreamSynchronize");
+  int64_t taken = c->t;                                // (set, and not yet on the device)
+  if (!c->step_dirty) ADAMW_CHK(hipMemcpy(&taken, &c->step_dev()->t, sizeof(taken), hipMemcpyDeviceToHost), "hipMemcpy");
+  *t = taken;
   return LORDO_OK;
 }
 

@@ -26,7 +26,7 @@ EXPORTS = [
     "lordo_get_stable_rank", "lordo_spectral_gap", "lordo_init_static",
     "lordo_adamw_workspace_bytes", "lordo_adamw_init", "lordo_adamw_step", "lordo_adamw_sync_payload",
     "lordo_adamw_export_moments", "lordo_adamw_import_moments", "lordo_adamw_get_step", "lordo_adamw_set_step",
-    "lordo_adamw_poll_status", "lordo_adamw_destroy", "lordo_grad_norm",
+    "lordo_adamw_steps_taken", "lordo_adamw_poll_status", "lordo_adamw_destroy", "lordo_grad_norm",
     "lordo_embed_lookup", "lordo_embed_workspace_bytes", "lordo_embed_gradient", "lordo_embed_gradient_rows",
 ]
 STATIC_WORKSPACE_BYTES = 64 << 20
@@ -132,6 +132,7 @@ def load() -> C.CDLL:
     lib.lordo_adamw_import_moments.argtypes = [vp, vp, vp]
     lib.lordo_adamw_get_step.argtypes = [vp, C.POINTER(C.c_int64)]
     lib.lordo_adamw_set_step.argtypes = [vp, C.c_int64]
+    lib.lordo_adamw_steps_taken.argtypes = [vp, C.POINTER(C.c_int64), vp]
     lib.lordo_adamw_poll_status.argtypes = [vp, vp]
     lib.lordo_adamw_destroy.argtypes = [vp]
     lib.lordo_adamw_destroy.restype = None
@@ -609,6 +610,13 @@ class AdamW:
     @step.setter
     def step(self, t):
         _check(self.lib.lordo_adamw_set_step(self.ctx, int(t)))
+
+    def steps_taken(self):
+        """Steps that the device has counted, replays among them and steps left out not (`step` counts the calls): what to save beside the moments
+        and to set `step` to when a run goes on from them.  Synchronises."""
+        t = C.c_int64(0)
+        _check(self.lib.lordo_adamw_steps_taken(self.ctx, C.byref(t), self._stream()))
+        return t.value
 
     def poll_status(self):
         """Raises (ENUMERIC) if a step was left out since the last poll because the clip coefficient, or grad_scale times it, was not finite."""

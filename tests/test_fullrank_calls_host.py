@@ -15,3 +15,7 @@ def _bytes(**hp):
 def test_weight_decay_has_a_limit(decay, code):
     """It meets the weights in fp32, divided by what the bias corrections make of the learning rate."""
     assert _bytes(weight_decay=decay) == code
+
+
+def test_steps_taken_needs_a_context():
+    assert lordo.load().lordo_adamw_steps_taken(None, C.byref(C.c_int64(0)), None) == lordo.EINVAL
