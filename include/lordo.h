@@ -402,8 +402,9 @@ int lordo_adamw_init(lordo_adamw** out, const lordo_tensor* tensors, int32_t n, 
  *   clip  device, two floats as lordo_grad_norm leaves them, or NULL (coefficient 1).  With a coefficient that is not finite, or not as the
  *         fp32 number grad_scale * clip[1], the whole step is left out -- weights, moments and the step count on the device stay -- and
  *         latched for lordo_adamw_poll_status.
- * The step count is kept as that of lordo_local_step: a recorded call counts its replays; lr and grad_scale are those of the recording.  A
- * step beside a lordo_local_step shares nothing with it. */
+ * The step count is kept as that of lordo_local_step: a recorded call counts its replays; lr and grad_scale are those of the recording.  The
+ * step after lordo_adamw_set_step cannot be the recorded one (LORDO_ESTATE): every replay would set the count again.  A step beside a
+ * lordo_local_step shares nothing with it. */
 int lordo_adamw_step(lordo_adamw* ctx, void* const* W, const lordo_grad* G, double lr, double grad_scale, const float* clip, void* stream);
 
 /* The moments as one fp32 array [u | v]: tensor i begins, in each half, at the sum of the sizes before it, each rounded up to 128 elements;

@@ -844,6 +844,12 @@ int lordo_adamw_step(lordo_adamw* c, void* const* W, const lordo_grad* G, double
   if ((reinterpret_cast<uintptr_t>(clip) & 3) != 0) return LORDO_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (c->step_dirty) {
+    // not into a recording, where every replay would set the count again
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
+      (void)hipGetLastError();
+      return LORDO_ESTATE;
+    }
     ADAMW_CHK(launch_adamw_set(c->step_dev(), c->hp.beta1, c->hp.beta2, c->hp.bias_correction, c->t, s), "k_adamw_set");
     c->step_dirty = false;      // (a call that fails below leaves the device count right: the last launch alone moves it on)
   }

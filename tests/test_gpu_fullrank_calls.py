@@ -111,3 +111,34 @@ def test_a_run_goes_on_from_the_steps_taken(torch, state):
         assert all(torch.equal(a, b) for a, b in zip(W, V)) and torch.equal(opt.export_moments(), other.export_moments())
     assert opt.steps_taken() == other.steps_taken() == 13
     graph.reset()
+
+
+def test_the_step_that_sets_the_count_is_not_recorded(torch):
+    """Every replay would set it again.  Refused with nothing enqueued; behind a step that was issued a recording counts on from what was set."""
+    from paper_2602_04396_amd import lordo
+    opt, twin = (lordo.AdamW([(5, 130)], lordo.adamw_hparams(), torch) for _ in range(2))
+    W, G = [torch.ones(5, 130, device="cuda")], [torch.randn(5, 130, device="cuda")]
+    V = [W[0].clone()]
+    opt.step = twin.step = 300
+    lists = opt.ptrs(W), lordo.grad_list(G)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        G[0].add_(0.0)                                   # (a graph of something)
+        with pytest.raises(lordo.LordoError) as e:
+            opt.local_step(*lists, 1e-2)
+    assert e.value.code == lordo.ESTATE and opt.step == opt.steps_taken() == 300
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(W[0], V[0])
+    opt.local_step(*lists, 1e-2)
+    again = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(again):
+        opt.local_step(*lists, 1e-2)
+    for _ in range(3):
+        again.replay()
+    for _ in range(4):
+        twin.local_step(V, G, 1e-2)
+    assert opt.steps_taken() == twin.steps_taken() == 304
+    assert torch.equal(W[0], V[0]) and torch.equal(opt.sync_payload(), twin.sync_payload())
+    graph.reset()
+    again.reset()
