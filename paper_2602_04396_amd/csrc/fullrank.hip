@@ -22,7 +22,10 @@ constexpr int GROUP_ROWS = 8;
 // Elements of a workgroup of the norm at a time: 16384, or 2048 where those would be less than one for each of its 1024 workgroups.
 constexpr int64_t NORM_CHUNK = 16384, NORM_SMALL_CHUNK = 2048;
 constexpr int NORM_BLOCKS = 1024;
-constexpr int64_t NORM_ALONE = 98304;    // elements of dense gradients that one workgroup takes without a second launch
+// Chunks of 16384 of dense gradients, at least one a tensor, that one workgroup takes without a second launch.  It takes them one after the other, 1.0 us each (short
+// ones) to 1.2.  Calls in a row in us: to 5 chunks 7.1, 6 8.2, 7 9.1, 8 10.0, 49 49, 200 vectors of 400 190; two launches 9.2 to 10.7.  In a recorded graph, without the
+// host, two launches are 5.3 to 5.6 and ahead from 4 chunks on (4 6.3, 6 8.2).
+constexpr int64_t NORM_ALONE = 6;
 constexpr int COUNTERS = 16;             // of finished workgroups, 128 bytes apart, behind them the one of finished counters
 
 // What the plan knows of a tensor (device memory, written once).
@@ -616,7 +619,7 @@ __device__ __forceinline__ double squares_of_rows(const void* g, const int32_t* 
 }
 
 // HBM: 1.3e9 bf16 elements in 218 tensors 425 us with the launch of k_norm_sum (5 us), 6.1 TB/s (with one request of 8 bytes in flight a thread and 64 tensors a
-// launch 975).  Few elements are one launch of one workgroup: 37000 fp32 ones 7 us, in two launches 10.
+// launch 975).  Few chunks are one launch of one workgroup: see NORM_ALONE.
 __global__ __launch_bounds__(1024) void k_norm_part(NormArgs a) {
   __shared__ double sums[16];
   double sum = 0.0;
@@ -953,24 +956,22 @@ int lordo_grad_norm(const lordo_grad* G, int32_t n, double max_norm, float* out,
   if ((reinterpret_cast<uintptr_t>(out) & 3) != 0 || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return LORDO_EINVAL;
   if (workspace_bytes < LORDO_NORM_WORKSPACE_BYTES) return LORDO_ENOMEM;
   auto elements = [](const lordo_grad& g) { return g.index ? g.slots * g.cols : g.rows * g.cols; };
-  int64_t all = 0, chunk = NORM_CHUNK, chunks = 0;
+  int64_t chunk = NORM_CHUNK, chunks = 0;
   bool by_rows = false;
   for (int i = 0; i < n; ++i) {
     if (!good_grad(G[i])) return LORDO_EINVAL;
-    all += elements(G[i]);
     by_rows |= G[i].index != nullptr;
     chunks += (elements(G[i]) + chunk - 1) / chunk;
     if (chunks > (int64_t(1) << 30)) return LORDO_EINVAL;
   }
-  if (chunks < NORM_BLOCKS) {
+  const bool one = chunks <= NORM_ALONE && !by_rows;             // (so no more tensors than a launch takes)
+  if (chunks < NORM_BLOCKS && !one) {
     chunk = NORM_SMALL_CHUNK;
     chunks = 0;
     for (int i = 0; i < n; ++i) chunks += (elements(G[i]) + chunk - 1) / chunk;
   }
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int blocks = (int)std::min<int64_t>(std::max<int64_t>(chunks, 1), NORM_BLOCKS);      // of every launch: each adds to the sums of the one before
-  const bool one = n <= GROUP && all <= NORM_ALONE && !by_rows;
-  if (one) chunk = NORM_CHUNK;
   NormArgs a;
   a.part = reinterpret_cast<double*>(workspace);
   a.max_norm = max_norm;
@@ -996,7 +997,7 @@ int lordo_grad_norm(const lordo_grad* G, int32_t n, double max_norm, float* out,
       a.chunks += (int32_t)mine;
     }
     at += a.count;
-    if (one && at == n && !a.add) {
+    if (one) {
       a.out = out;
       hipLaunchKernelGGL(k_norm_part, dim3(1), dim3(1024), 0, s, a);
       return launched("k_norm_part");

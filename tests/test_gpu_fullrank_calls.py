@@ -142,3 +142,41 @@ def test_the_step_that_sets_the_count_is_not_recorded(torch):
     assert torch.equal(W[0], V[0]) and torch.equal(opt.sync_payload(), twin.sync_payload())
     graph.reset()
     again.reset()
+
+
+def test_many_small_gradients_are_not_summed_one_after_the_other(torch):
+    """The norm of 200 vectors takes no longer than that of 201, which are more than a launch holds and take 8.5 us in three of them; one workgroup that walks
+    over 200 takes 190.  Four times that leaves room for the clock."""
+    from paper_2602_04396_amd import lordo
+    us = []
+    for n in (200, 201):
+        G, out = lordo.grad_list([torch.ones(400, device="cuda") for _ in range(n)]), torch.empty(2, device="cuda")
+        lordo.grad_norm(G, 1.0, out=out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(20):
+                lordo.grad_norm(G, 1.0, out=out)
+        times = []
+        for _ in range(9):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            graph.replay()
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b) * 50)
+        assert abs(float(out[0]) - (400 * n) ** 0.5) <= 1.01 * ref.EPS32 * (400 * n) ** 0.5
+        us.append(sorted(times)[4])
+        graph.reset()
+    assert us[0] <= 4 * us[1], us
+
+
+@pytest.mark.parametrize("sizes", [[16384] * 6, [16384] * 6 + [1], [1] * 6, [1] * 7, [98304], [98305], [16385] * 3, [16385] * 3 + [5], [7] * 200])
+def test_norm_on_both_sides_of_one_launch(torch, sizes):
+    from paper_2602_04396_amd import lordo
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for dtype in (torch.float32, torch.bfloat16):
+        G = [torch.randn(n, generator=gen, device="cuda").to(dtype) for n in sizes]
+        want = sum(float((g.double() ** 2).sum()) for g in G) ** 0.5
+        for out in (lordo.grad_norm(G, 0.5 * want), lordo.grad_norm(G[::-1], 0.5 * want)):
+            assert abs(float(out[0]) - want) <= 1.01 * ref.EPS32 * want and abs(float(out[1]) - 0.5) <= 1.01 * ref.EPS32
