@@ -21,6 +21,7 @@ constexpr int RANK_ROW = 32;          // tokens that a workgroup of it ranks
 constexpr int PLACE_CHUNK = 2048;     // tokens that a workgroup of k_place has in registers
 constexpr int PLACE_BLOCKS = 256;     // most workgroups of a digit
 constexpr int MAX_BINS = 512;
+constexpr int64_t LOOKUP_TOKENS = 1 << 23;   // most tokens of a launch of k_lookup: a launch has less than 2^32 threads, and long rows are a workgroup each
 
 struct Ids {
   const void* p;
@@ -34,34 +35,26 @@ __device__ __forceinline__ int32_t token_key(const Ids& ids, int64_t t) {
   return id < 0 || id >= ids.vocab || id == ids.pad_id ? ids.vocab : (int32_t)id;
 }
 
-// A thread copies eight columns of ROWS rows, all requested before the first is written.  NARROW: rows shorter than that, a thread an element.
-// Memory: 32768 tokens, an eighth of them padding, of a 32000 x 2048 fp32 table to bf16 49 us: 134 MB written and 235 read, two thirds of that from the caches (four
-// columns of one row a thread: 58 us).
-template <bool IN_BF, bool OUT_BF, int ROWS, bool NARROW>
+// A thread copies eight columns of a row.  NARROW: rows shorter than that, a thread an element.
+// Memory: 32768 tokens, an eighth of them padding, of a 32000 x 2048 fp32 table to bf16 48 us: 134 MB written and 235 read, two thirds of that from the caches.
+// Four columns a thread took 58.  Four rows a thread, all requested before the first is written, took 49, and were 0 to 25 % slower from 512 workgroups of one row to 32768,
+// tables of both types, 64 to 4096 columns: the many workgroups keep enough in flight.
+template <bool IN_BF, bool OUT_BF, bool NARROW>
 __global__ __launch_bounds__(256) void k_lookup(const void* table, Ids ids, int64_t tokens, int64_t cols, int lanes_log2, float scale, void* out) {
   constexpr int VEC = NARROW ? 1 : 8;
-  const int lanes = 1 << lanes_log2, per = 256 >> lanes_log2;          // threads of a row, rows of a workgroup at a time
+  const int lanes = 1 << lanes_log2, per = 256 >> lanes_log2;          // threads of a row, rows of a workgroup
   const int64_t c0 = ((int64_t)blockIdx.y * lanes + (threadIdx.x & (lanes - 1))) * VEC;
-  if (c0 >= cols) return;
+  const int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> lanes_log2);
+  if (c0 >= cols || row >= tokens) return;
   const int64_t c = std::min(c0, cols - VEC);                          // the last piece of a row ends where the row does
-  const int64_t first = (int64_t)blockIdx.x * per * ROWS + (threadIdx.x >> lanes_log2);
-  int32_t id[ROWS];
-  Piece<IN_BF, VEC> x[ROWS];
+  const int32_t id = token_key(ids, row);
+  Piece<IN_BF, VEC> x;
+  x.clear();
+  if (id < ids.vocab) x.load(table, (int64_t)id * cols + c);
+  float y[VEC];
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) id[r] = first + r * per < tokens ? token_key(ids, first + r * per) : ids.vocab;
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    x[r].clear();
-    if (id[r] < ids.vocab) x[r].load(table, (int64_t)id[r] * cols + c);
-  }
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    if (first + r * per >= tokens) break;
-    float y[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) y[e] = x[r].value(e) * scale;
-    put_piece<OUT_BF, VEC>(out, (first + r * per) * cols + c, y, (int)(c0 - c));
-  }
+  for (int e = 0; e < VEC; ++e) y[e] = x.value(e) * scale;
+  put_piece<OUT_BF, VEC>(out, row * cols + c, y, (int)(c0 - c));
 }
 
 struct Sorted { int32_t *key, *pos; };
@@ -402,13 +395,15 @@ void launch_lookup_as(const void* table, Ids ids, int64_t tokens, int64_t cols, 
   int lanes_log2 = 0;
   while (lanes_log2 < 8 && (int64_t(1) << lanes_log2) < pieces) ++lanes_log2;
   const int64_t per = 256 >> lanes_log2, columns = (pieces + (int64_t(1) << lanes_log2) - 1) >> lanes_log2;
-  // four rows a thread once that leaves eight workgroups a compute unit
-  const int rows = (tokens + per - 1) / per * columns >= 8192 ? 4 : 1;
-  const dim3 grid((unsigned)((tokens + per * rows - 1) / (per * rows)), (unsigned)columns), block(256);
-  if (narrow && rows == 4) hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, 4, true>), grid, block, 0, s, table, ids, tokens, cols, lanes_log2, scale, out);
-  else if (narrow) hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, 1, true>), grid, block, 0, s, table, ids, tokens, cols, lanes_log2, scale, out);
-  else if (rows == 4) hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, 4, false>), grid, block, 0, s, table, ids, tokens, cols, lanes_log2, scale, out);
-  else hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, 1, false>), grid, block, 0, s, table, ids, tokens, cols, lanes_log2, scale, out);
+  for (int64_t at = 0; at < tokens; at += LOOKUP_TOKENS) {
+    const int64_t n = std::min(tokens - at, LOOKUP_TOKENS);
+    Ids part = ids;
+    part.p = reinterpret_cast<const char*>(ids.p) + at * (ids.wide ? 8 : 4);
+    void* const to = reinterpret_cast<char*>(out) + at * cols * (OUT_BF ? 2 : 4);
+    const dim3 grid((unsigned)((n + per - 1) / per), (unsigned)columns), block(256);
+    if (narrow) hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, true>), grid, block, 0, s, table, part, n, cols, lanes_log2, scale, to);
+    else hipLaunchKernelGGL((k_lookup<IN_BF, OUT_BF, false>), grid, block, 0, s, table, part, n, cols, lanes_log2, scale, to);
+  }
 }
 void launch_lookup(const void* table, bool in_bf, Ids ids, int64_t tokens, int64_t cols, float scale, void* out, bool out_bf, hipStream_t s) {
   if (in_bf && out_bf) launch_lookup_as<true, true>(table, ids, tokens, cols, scale, out, s);

@@ -1,4 +1,4 @@
-"""Token embedding at the sizes of real batches: four rows a thread in the lookup, tiles of 16 and 32 tokens in the gradient, arrays beyond 2^31 elements.
+"""Token embedding at the sizes of real batches: lookups of thousands of workgroups, tiles of 16 and 32 tokens in the gradient, arrays beyond 2^31 elements.
 Gradients of whole numbers below 2^24 are summed exactly in fp32, so every form has to give the sum itself."""
 import numpy as np
 import pytest
@@ -29,7 +29,7 @@ def _ids(torch, kind, tokens, vocab, gen):
     return ids
 
 
-# tokens, cols: workgroups of one row a thread, from 8192 on four rows
+# 2 to 32771 workgroups of 1 to 256 rows, ragged ones among them
 @pytest.mark.parametrize("tokens, cols", [(4095, 2049), (4101, 2049), (2050, 8200), (8191, 1031), (16390, 1031), (262147, 5), (262147, 8), (524300, 20), (32771, 512)])
 @pytest.mark.parametrize("w_bf16, out_bf16", [(False, False), (False, True), (True, False), (True, True)])
 def test_lookup_of_large_batches(torch, tokens, cols, w_bf16, out_bf16):
@@ -133,3 +133,19 @@ def test_batches_beyond_32_bits(torch):
     slot = r.index[:vocab].long()
     assert int(slot.min()) >= 0 and int(slot.max()) * cols > 1 << 30
     assert torch.equal(r.rows[slot], out)
+
+
+@pytest.mark.parametrize("wide", [True, False])
+def test_lookup_of_more_tokens_than_a_launch_takes(torch, wide):
+    """Rows of more than 1024 columns are a workgroup each, 256 threads: 2^23 of them are one launch."""
+    from paper_2602_04396_amd import lordo
+    tokens, cols, vocab = (1 << 23) + 5, 1032, 50
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    table = torch.randn(vocab, cols, generator=gen, device="cuda").bfloat16()
+    ids = torch.randint(-1, vocab, (tokens,), generator=gen, device="cuda", dtype=torch.int64 if wide else torch.int32)
+    out = torch.full((tokens, cols), 7.0, dtype=torch.bfloat16, device="cuda")
+    lordo.embed_lookup(table, ids, out=out)
+    padded = torch.cat([table, torch.zeros(1, cols, dtype=torch.bfloat16, device="cuda")])      # (the row -1)
+    step = 1 << 19
+    for at in list(range(0, tokens, step)):
+        assert torch.equal(out[at:at + step], padded[ids[at:at + step].long()])
