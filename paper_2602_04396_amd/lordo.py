@@ -520,10 +520,13 @@ class AdamW:
         self.lib, self.torch, self.hp = load(), torch, hp
         self.ctx = C.c_void_p()
         self.shapes = [tuple(sh) for sh in shapes]
-        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        current = torch.device("cuda", torch.cuda.current_device())
+        self.device = current if device is None else torch.device(device)
+        if self.device == torch.device("cuda"):          # ("cuda" without a number: the current one)
+            self.device = current
         self.made_for = (self.device, hp.param_dtype, tuple(sh[:2] for sh in self.shapes))
         self.at = self.device.index
-        if self.at != torch.cuda.current_device():
+        if self.device != current:
             raise ValueError(f"{self.device} is not the current device")
         arr = (Tensor * len(self.shapes))()
         for a, sh in zip(arr, self.shapes):

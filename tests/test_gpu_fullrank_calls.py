@@ -180,3 +180,17 @@ def test_norm_on_both_sides_of_one_launch(torch, sizes):
         want = sum(float((g.double() ** 2).sum()) for g in G) ** 0.5
         for out in (lordo.grad_norm(G, 0.5 * want), lordo.grad_norm(G[::-1], 0.5 * want)):
             assert abs(float(out[0]) - want) <= 1.01 * ref.EPS32 * want and abs(float(out[1]) - 0.5) <= 1.01 * ref.EPS32
+
+
+def test_the_device_of_a_context(torch):
+    """The current one, by its number or without; another is refused."""
+    from paper_2602_04396_amd import lordo
+    for device in (None, "cuda", torch.device("cuda"), "cuda:0", torch.device("cuda", 0), 0):
+        opt = lordo.AdamW([(4, 8)], lordo.adamw_hparams(), torch, device=device)
+        assert opt.device == torch.device("cuda", 0)
+        W = [torch.ones(4, 8, device="cuda")]
+        opt.local_step(W, [torch.ones(4, 8, device="cuda")], 1e-2)
+        assert torch.all(W[0] < 1.0)
+    for device in ("cpu", "cuda:1"):
+        with pytest.raises(ValueError):
+            lordo.AdamW([(4, 8)], lordo.adamw_hparams(), torch, device=device)
