@@ -156,11 +156,13 @@ def _check(code):
 
 class PtrList:
     """Pointer array of an already validated tensor list, reusable across calls (keeps the
-    tensors alive).  Built by Lordo.ptrs(); lets a tight loop skip per-call validation."""
+    tensors alive).  Built by Lordo.ptrs() and AdamW.ptrs() (`made_for`: its shapes, type and
+    device); lets a tight loop skip per-call validation."""
 
-    def __init__(self, tensors, arr):
+    def __init__(self, tensors, arr, made_for=None):
         self.tensors = tensors
         self.arr = arr
+        self.made_for = made_for
 
 
 def _ptr_array(tensors):
@@ -222,6 +224,8 @@ class Lordo:
 
     def _check_tensors(self, ts, dtype, kind, allow_none=False):
         if isinstance(ts, PtrList):
+            if ts.made_for is not None or len(ts.tensors) != self.n:      # AdamW's, or another set's: the library reads n pointers
+                raise ValueError("a list of tensors made for other shapes")
             return
         if len(ts) != self.n:
             raise ValueError("one tensor per matrix expected")
@@ -543,7 +547,7 @@ class AdamW:
     def ptrs(self, W) -> PtrList:
         """Validate the list of weights once and freeze its pointers for repeated calls."""
         if isinstance(W, PtrList):
-            if getattr(W, "made_for", None) != self.made_for:
+            if W.made_for != self.made_for:
                 raise ValueError("a list of weights made for other shapes")
             return W
         dtype = self.torch.bfloat16 if self.hp.param_dtype == BF16 else self.torch.float32
@@ -555,9 +559,7 @@ class AdamW:
         spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in W)
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("two of the weights overlap: a tensor is stepped once")
-        p = PtrList(list(W), _ptr_array(W))
-        p.made_for = self.made_for
-        return p
+        return PtrList(list(W), _ptr_array(W), self.made_for)
 
     def local_step(self, W, G, lr, grad_scale=1.0, clip=None):
         """One step; the gradient is grad_scale * clip[1] * G (clip: what grad_norm returned, or None)."""

@@ -19,3 +19,16 @@ def test_weight_decay_has_a_limit(decay, code):
 
 def test_steps_taken_needs_a_context():
     assert lordo.load().lordo_adamw_steps_taken(None, C.byref(C.c_int64(0)), None) == lordo.EINVAL
+
+
+def test_the_low_rank_context_refuses_lists_made_for_others():
+    """The library reads a pointer for each of its matrices, so a shorter list would be read beyond its end."""
+    import torch
+    low = lordo.Lordo.__new__(lordo.Lordo)
+    low.shapes, low.n, low.ctx = [(4, 8, 2), (8, 4, 2)], 2, C.c_void_p()
+    two = [torch.zeros(4, 8), torch.zeros(8, 4)]
+    low._check_tensors(lordo.PtrList(two, lordo._ptr_array(two)), torch.float32, "pq")
+    for bad in (lordo.PtrList(two[:1], lordo._ptr_array(two[:1])),
+                lordo.PtrList(two, lordo._ptr_array(two), (torch.device("cuda", 0), lordo.F32, ((4, 8), (8, 4))))):
+        with pytest.raises(ValueError):
+            low._check_tensors(bad, torch.float32, "pq")
