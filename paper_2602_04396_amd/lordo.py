@@ -648,7 +648,8 @@ def _ids(ids, torch):
 
 
 def embed_lookup(table, ids, scale=1.0, out=None, dtype=None):
-    """out[...] = scale * table[ids[...]] as a tensor of ids.shape + (cols,), of `dtype` (the table's if None); zeros for ids outside [0, vocab)."""
+    """out[...] = scale * table[ids[...]] as a tensor of ids.shape + (cols,), of `dtype` (the table's if None); zeros for ids outside [0, vocab).
+    Autograd does not see it, also where the table requires a gradient: the output has none, its gradient goes to embed_gradient or embed_gradient_rows."""
     torch = _torch()
     if table.dim() != 2 or not table.is_contiguous():
         raise ValueError("expected a contiguous (vocab, cols) table")
