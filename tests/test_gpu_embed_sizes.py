@@ -50,9 +50,13 @@ def test_lookup_of_large_batches(torch, tokens, cols, w_bf16, out_bf16):
 
 
 def _sum(torch, ids, dy, vocab):
+    """Sums by differences of the running sum over the sorted ids, exact for whole numbers (adding by atomics to one id takes minutes)."""
     there = (ids >= 0) & (ids < vocab)
-    out = torch.zeros(vocab, dy.shape[1], device="cuda", dtype=torch.float64)
-    return out.index_add_(0, ids[there].long(), dy[there].double())
+    keys, order = torch.sort(ids[there].long())
+    run = torch.zeros(len(keys) + 1, dy.shape[1], dtype=torch.float64, device="cuda")
+    torch.cumsum(dy[there].double()[order], 0, out=run[1:])
+    ends = torch.searchsorted(keys, torch.arange(vocab + 1, device="cuda"))
+    return run[ends[1:]] - run[ends[:-1]]
 
 
 # 9000 x 1030: tiles of 8 (bf16) and 16 (fp32); 65539: 16; 131075: 32; 20000 x 2100: 32
@@ -65,7 +69,9 @@ def test_gradient_of_large_batches(torch, tokens, vocab, cols, kind):
     whole = torch.randint(-8, 9, (tokens, cols), generator=gen, device="cuda")
     base = torch.randint(-100, 101, (vocab, cols), generator=gen, device="cuda").double()
     total = _sum(torch, ids, whole, vocab)
-    none = torch.bincount(ids[(ids >= 0) & (ids < vocab)], minlength=vocab) == 0
+    none = torch.ones(vocab + 1, dtype=torch.bool, device="cuda")
+    none[torch.where((ids >= 0) & (ids < vocab), ids, vocab)] = False
+    none = none[:vocab]
     for dtype in (torch.float32, torch.bfloat16):
         dy = whole.to(dtype)
         dy[(ids < 0) | (ids >= vocab)] = float("nan")              # what takes no part is not looked at
@@ -149,3 +155,78 @@ def test_lookup_of_more_tokens_than_a_launch_takes(torch, wide):
     step = 1 << 19
     for at in list(range(0, tokens, step)):
         assert torch.equal(out[at:at + step], padded[ids[at:at + step].long()])
+
+
+@pytest.mark.parametrize("rows", [False, True])
+@pytest.mark.parametrize("tokens, vocab, cols", [(300, 50, 40), (9001, 700, 130), (70001, 32000, 64)])
+def test_recorded_gradients_follow_their_tokens(torch, tokens, vocab, cols, rows):
+    """Recorded on a side stream, two graphs with their own workspaces, replayed in turn over new tokens: ranked in one launch, by digits, long runs and none."""
+    from paper_2602_04396_amd import lordo
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    state = []
+    for k in range(2):
+        s = dict(ids=torch.zeros(tokens, dtype=torch.int64, device="cuda"), dy=torch.zeros(tokens, cols, device="cuda"), out=torch.zeros(vocab, cols, device="cuda"))
+        s["rows"] = lordo.RowGrad(torch.zeros(tokens, cols, device="cuda"), torch.zeros(vocab + tokens, dtype=torch.int32, device="cuda"), vocab)
+        state.append(s)
+
+    def call(s):
+        if rows:
+            lordo.embed_gradient_rows(s["ids"], s["dy"], vocab, out=s["rows"])
+        else:
+            lordo.embed_gradient(s["ids"], s["dy"], s["out"])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    with torch.cuda.stream(side):
+        for s in state:
+            call(s)
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                call(s)
+            graphs.append(g)
+    torch.cuda.current_stream().wait_stream(side)
+    for kind in ("zipf", "all", "mixed", "pairs", "zipf"):
+        want = []
+        for s in state:
+            s["ids"].copy_(_ids(torch, kind, tokens, vocab, gen))
+            s["dy"].copy_(torch.randint(-8, 9, (tokens, cols), generator=gen, device="cuda"))
+            want.append(_sum(torch, s["ids"], s["dy"], vocab).float())
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for s, w in zip(state, want):
+            if rows:
+                slot = s["rows"].index[:vocab].long()
+                got = torch.where((slot >= 0)[:, None], s["rows"].rows[slot.clamp(min=0)], 0.0)
+                there = torch.zeros(vocab + 1, dtype=torch.bool, device="cuda")
+                there[torch.where((s["ids"] >= 0) & (s["ids"] < vocab), s["ids"], vocab)] = True
+                there = there[:vocab]
+                assert torch.equal(slot >= 0, there) and torch.equal(got, w)
+            else:
+                assert torch.equal(s["out"], w)
+    for g in graphs:
+        g.reset()
+
+
+@pytest.mark.parametrize("kind", ["zipf", "all", "mixed"])
+def test_the_most_tokens_and_the_largest_vocabulary(torch, kind):
+    from paper_2602_04396_amd import lordo
+    tokens, vocab, gen = lordo.MAX_TOKENS, lordo.MAX_VOCAB, torch.Generator(device="cuda").manual_seed(7)
+    ids = _ids(torch, kind, tokens, vocab, gen)
+    dy = torch.randint(0, 2, (tokens, 1), generator=gen, device="cuda").bfloat16()
+    dy -= 0.5                                            # (halves: sums below 2^24 of them are exact)
+    there = (ids >= 0) & (ids < vocab)
+    want, held = _sum(torch, ids, dy, vocab)[:, 0].float(), torch.zeros(vocab, dtype=torch.bool, device="cuda")
+    held[ids[there]] = True
+    out = lordo.embed_gradient(ids, dy, torch.full((vocab, 1), 9.0, device="cuda"))
+    assert torch.equal(out[:, 0], want)
+    r = lordo.embed_gradient_rows(ids.int(), dy, vocab)
+    slot = r.index[:vocab].long()
+    assert torch.equal(slot >= 0, held)
+    assert torch.equal(torch.where(slot >= 0, r.rows[slot.clamp(min=0), 0], 0.0), want)
+    norm = float((want.double() ** 2).sum()) ** 0.5
+    assert abs(float(lordo.grad_norm([r])[0]) - norm) <= 1.01 * 2.0 ** -24 * norm
+    for bad in (ids.repeat(2)[:tokens + 1], ):
+        with pytest.raises(lordo.LordoError):
+            lordo.embed_gradient_rows(bad, torch.zeros(tokens + 1, 1, device="cuda"), vocab)

@@ -272,3 +272,41 @@ def test_gradient_by_rows_beyond_32_bits(torch):
     assert all(torch.equal(a, b) for a, b in zip(*results))
     want = math.sqrt(float((dense.double() ** 2).sum()))
     assert abs(float(lordo.grad_norm([r])[0]) - want) <= 1.01 * ref.EPS32 * want
+
+
+@pytest.mark.parametrize("state", ["f32", "q8"])
+def test_recorded_steps_of_large_sets(torch, state):
+    """Many tensors in two launches, one of them by rows, with its norm: replays beside the same steps issued, synchronised in between."""
+    from paper_2602_04396_amd import lordo
+    shapes = [(1, 16400 + 37 * k, k % 2) for k in range(230)] + [(9001, 60)]
+    gen = _gen(torch, 16)
+    hp = lordo.adamw_hparams(weight_decay=0.1, param_dtype=lordo.BF16, state_dtype=lordo.Q8 if state == "q8" else lordo.F32)
+    W = [_tensor(torch, gen, sh[0], sh[1], torch.bfloat16, 0.02) for sh in shapes]
+    V = [w.clone() for w in W]
+    G = [_tensor(torch, gen, sh[0], sh[1], torch.float32, 1.0) for sh in shapes[:-1]]
+    ids, dy = torch.zeros(12000, dtype=torch.int64, device="cuda"), torch.zeros(12000, 60, device="cuda")
+    eager, twin = lordo.AdamW(shapes, hp, torch), lordo.AdamW(shapes, hp, torch)
+    PW, PV = eager.ptrs(W), twin.ptrs(V)
+
+    def step(opt, weights):
+        grads = G + [lordo.embed_gradient_rows(ids, dy, 9001)]
+        clip = lordo.grad_norm(grads, 1.0)
+        opt.local_step(weights, grads, 1e-2, clip=clip)
+        return clip
+
+    step(lordo.AdamW(shapes, hp, torch), [w.clone() for w in W])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded = step(twin, PV)
+    for k in range(4):
+        ids.copy_(torch.randint(-1, 9001, ids.shape, generator=gen, device="cuda"))
+        dy.copy_(torch.randn(dy.shape, generator=gen, device="cuda"))
+        for g in G:
+            g.copy_(torch.randn(g.shape, generator=gen, device="cuda"))
+        clip = step(eager, PW)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(clip, recorded) and all(torch.equal(a, b) for a, b in zip(W, V))
+        assert torch.equal(eager.export_moments(), twin.export_moments()) and eager.steps_taken() == twin.steps_taken() == k + 1
+    graph.reset()
