@@ -19,8 +19,10 @@ constexpr int64_t ADAMW_CHUNK = 4096, ADAMW_SMALL_CHUNK = 1024, ADAMW_MANY = 102
 constexpr int Q8_BLOCK = 128;            // elements that share an exponent
 constexpr int GROUP = 200;               // tensors of one launch, and gradients by rows among them: their pointers travel in the kernel arguments (below 4 KiB)
 constexpr int GROUP_ROWS = 8;
-// Elements of a workgroup of the norm at a time: 16384, or 2048 where those would be less than one for each of its 1024 workgroups.
-constexpr int64_t NORM_CHUNK = 16384, NORM_SMALL_CHUNK = 2048;
+// Elements of a workgroup of the norm at a time: 16384, or 2048 where those would be less than 320 (256 compute units).  In us, 2048 and 16384: one tensor of 500000 fp32
+// elements 5.7 and 6.4, 4000000 7.7 and 7.1, 16000000 18.0 and 15.0; bf16 5.7 and 6.1, 8.5 and 6.3, 17.2 and 8.8; 150 tensors of 10000 6.2 and 6.0, of 20000 13.4 and 6.7;
+// short rows, the last to gain: of 768, 128 chunks of 16384 7.6 and 10.3, 256 9.8 and 10.5, 512 14.1 and 11.0.
+constexpr int64_t NORM_CHUNK = 16384, NORM_SMALL_CHUNK = 2048, NORM_MANY = 320;
 constexpr int NORM_BLOCKS = 1024;
 // Chunks of 16384 of dense gradients, at least one a tensor, that one workgroup takes without a second launch.  It takes them one after the other, 1.0 us each (short
 // ones) to 1.2.  Calls in a row in us: to 5 chunks 7.1, 6 8.2, 7 9.1, 8 10.0, 49 49, 200 vectors of 400 190; two launches 9.2 to 10.7.  In a recorded graph, without the
@@ -965,7 +967,7 @@ int lordo_grad_norm(const lordo_grad* G, int32_t n, double max_norm, float* out,
     if (chunks > (int64_t(1) << 30)) return LORDO_EINVAL;
   }
   const bool one = chunks <= NORM_ALONE && !by_rows;             // (so no more tensors than a launch takes)
-  if (chunks < NORM_BLOCKS && !one) {
+  if (chunks < NORM_MANY && !one) {
     chunk = NORM_SMALL_CHUNK;
     chunks = 0;
     for (int i = 0; i < n; ++i) chunks += (elements(G[i]) + chunk - 1) / chunk;

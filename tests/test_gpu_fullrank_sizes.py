@@ -188,7 +188,7 @@ def test_many_gradients_by_rows(torch, count):
         assert all(torch.equal(a, b) for a, b in zip(*results))
 
 
-@pytest.mark.parametrize("sizes", [[17000001, 5, 100003], [1024 * 16384], [1023 * 16384 + 1], [3 + 31 * k % 977 for k in range(201)], [1 + 17 * k % 5001 for k in range(650)],
+@pytest.mark.parametrize("sizes", [[17000001, 5, 100003], [320 * 16384], [319 * 16384], [319 * 16384 + 1], [1] * 319 + [16385], [1024 * 16384], [1023 * 16384 + 1], [3 + 31 * k % 977 for k in range(201)], [1 + 17 * k % 5001 for k in range(650)],
                                    [90000 + k for k in range(401)]])
 @pytest.mark.parametrize("bf16, shift", [(False, 0), (True, 0), (False, 1), (True, 3)])
 def test_norm_of_large_sets(torch, sizes, bf16, shift):
