@@ -336,6 +336,7 @@ int lordo_profile_read(lordo_ctx* ctx, int32_t kernel_class, double* total_ms, i
  *   - the calls without a context work on the GPU that is current, where all their arrays have to live;
  *   - a workspace is scratch between the start and the end of one call: calls that may run at the same time (two streams,
  *     two recorded graphs) need one each;
+ *   - an array that a call writes overlaps no other array of the call;
  *   - scale, grad_scale, lr and lr * weight_decay have to be finite as fp32 numbers.
  * ------------------------------------------------------------------------------------------------------------- */
 #define LORDO_Q8  2            /* moments in 8 bits, see lordo_adamw_hparams.state_dtype */
@@ -380,8 +381,9 @@ typedef struct {
                                     w / 2^17, w the upper 17 bits of x for u and the lower 17 for v, in 32 bits x = t 0x9E3779B1 + i 0xBB67AE85 for element
                                     i of its tensor at step t; x = (x xor x>>15) 0x6A09E667; x = x xor x>>14.  So it rounds up in the right share of
                                     the steps, and changes below the grid (1 - beta2 of v a step) add up.
-                                    v > 0 is never held as 0 (unless its block is 0 in fp32); u below its least value takes it by the same rule, or 0.  W is updated from the moments before this rounding.  An infinity, a NaN or more than 2^127
-                                    makes the moments of its whole block NaN */
+                                    v > 0 is never held as 0 (unless its block is 0 in fp32); u below its least value takes it by the same rule, or 0.
+                                    W is updated from the moments before this rounding.  An infinity, a NaN or more than 2^127 makes the moments
+                                    of its whole block NaN */
   int32_t reserved;              /* must be 0 */
 } lordo_adamw_hparams;
 
